@@ -1,6 +1,6 @@
 """ctypes binding of libmoe_offload.so: argument marshalling only.
 
-Function names and arguments mirror include/moe_offload.h one to one.  Every step of the
+Function names and arguments mirror include/moe_offload.h and include/moe_kv.h one to one.  Every step of the
 decode path runs inside the library; PyTorch appears here only as the owner of device
 memory, pinned host memory and streams (`Engine` below).
 """
@@ -27,6 +27,14 @@ EXPORTS = [
     "moe_stack_step", "moe_layer_resolve", "moe_layer_stats", "moe_layer_cache_state", "moe_layer_placement",
     "moe_layer_reset", "moe_ctx_read_y", "moe_ctx_profile_enable", "moe_ctx_profile_read", "moe_ctx_profile_timeline", "moe_ctx_set_option", "moe_probe_bandwidth", "moe_layer_set_prefetch", "moe_layer_set_flags", "moe_last_error", "moe_last_hip_error",
 ]
+
+# include/moe_kv.h
+MOE_KV_MAX_REQUESTS, MOE_KV_MAX_TOKENS = 4096, 1048576
+MOE_KV_E4M3, MOE_KV_INT8 = 0, 1
+MOE_KV_F16, MOE_KV_BF16 = 0, 1
+MOE_KV_SERVED, MOE_KV_NO_PAGES, MOE_KV_TOO_LONG, MOE_KV_BAD_SIZE = 0, 1, 2, 3
+KV_EXPORTS = ["moe_kv_plan_bytes", "moe_kv_scratch_bytes", "moe_kv_plan", "moe_kv_release", "moe_kv_write", "moe_kv_attend",
+              "moe_kv_gather"]
 
 
 class CtxConfig(C.Structure):
@@ -94,6 +102,34 @@ class Profile(C.Structure):
                     "total_ms": float(getattr(self, k).total_ms)} for k, _ in self._fields_}
 
 
+class KvCache(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_pages", "page", "kv_heads", "head_dim", "format", "reserved")] + [
+        (n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
+
+
+class KvStep(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_requests", "n_tokens", "max_new", "max_blocks", "n_pages", "page", "kv_heads",
+                                         "head_dim", "q_heads", "causal", "window", "reserved")]
+
+
+class KvLists(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("ctx_len", "new_len", "block_table", "free_pages", "free_count", "row_start",
+                                          "positions", "slots", "kv_len", "status", "free_left")]
+
+
+class KvRows(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("eps", C.c_float),
+                ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64),
+                ("q_gamma", C.c_void_p), ("k_gamma", C.c_void_p), ("inv_freq", C.c_void_p),
+                ("q_out", C.c_void_p), ("q_out_stride", C.c_int64)]
+
+
+class KvQuery(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("scale", C.c_float), ("q", C.c_void_p), ("q_stride", C.c_int64),
+                ("out", C.c_void_p), ("out_stride", C.c_int64), ("lse", C.c_void_p)]
+
+
 class MoeError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"moe_offload error {code}: {msg}")
@@ -151,7 +187,16 @@ def lib() -> C.CDLL:
     L.moe_layer_set_flags.argtypes = [vp, i32]
     L.moe_last_error.restype = C.c_char_p
     L.moe_last_hip_error.restype = i32
-    for name in EXPORTS:
+    L.moe_kv_plan_bytes.restype = u64
+    L.moe_kv_plan_bytes.argtypes = [C.POINTER(KvStep)]
+    L.moe_kv_scratch_bytes.restype = u64
+    L.moe_kv_scratch_bytes.argtypes = [C.POINTER(KvStep)]
+    L.moe_kv_plan.argtypes = [C.POINTER(KvStep), C.POINTER(KvLists), vp, vp]
+    L.moe_kv_release.argtypes = [vp, i32, i32, i32, i32, i32, vp, vp, vp, i32, vp, vp]
+    L.moe_kv_write.argtypes = [C.POINTER(KvCache), C.POINTER(KvStep), vp, C.POINTER(KvRows), vp]
+    L.moe_kv_attend.argtypes = [C.POINTER(KvCache), C.POINTER(KvStep), vp, vp, C.POINTER(KvQuery), vp, u64, vp]
+    L.moe_kv_gather.argtypes = [C.POINTER(KvCache), vp, i32, i32, vp, vp, vp]
+    for name in EXPORTS + KV_EXPORTS:
         fn = getattr(L, name)
         if fn.restype is C.c_int:
             fn.restype = i32
@@ -318,3 +363,34 @@ def moe_layer_set_prefetch(layer, m: int) -> None:
 
 def moe_layer_set_flags(layer, flags: int) -> None:
     check(lib().moe_layer_set_flags(layer, flags))
+
+
+def moe_kv_plan_bytes(step: KvStep) -> int:
+    return int(lib().moe_kv_plan_bytes(C.byref(step)))
+
+
+def moe_kv_scratch_bytes(step: KvStep) -> int:
+    return int(lib().moe_kv_scratch_bytes(C.byref(step)))
+
+
+def moe_kv_plan(step: KvStep, lists: KvLists, plan_dev: int, stream: int) -> None:
+    check(lib().moe_kv_plan(C.byref(step), C.byref(lists), plan_dev, stream))
+
+
+def moe_kv_release(requests: int, n: int, n_requests: int, n_pages: int, page: int, max_blocks: int, ctx_len: int,
+                   block_table: int, free_pages: int, capacity: int, free_count: int, stream: int) -> None:
+    check(lib().moe_kv_release(requests, n, n_requests, n_pages, page, max_blocks, ctx_len, block_table, free_pages, capacity,
+                               free_count, stream))
+
+
+def moe_kv_write(cache: KvCache, step: KvStep, plan_dev: int, rows: KvRows, stream: int) -> None:
+    check(lib().moe_kv_write(C.byref(cache), C.byref(step), plan_dev, C.byref(rows), stream))
+
+
+def moe_kv_attend(cache: KvCache, step: KvStep, plan_dev: int, block_table: int, query: KvQuery, scratch: Optional[int],
+                  scratch_bytes: int, stream: int) -> None:
+    check(lib().moe_kv_attend(C.byref(cache), C.byref(step), plan_dev, block_table, C.byref(query), scratch, scratch_bytes, stream))
+
+
+def moe_kv_gather(cache: KvCache, slots: int, n: int, dtype: int, k_out: int, v_out: int, stream: int) -> None:
+    check(lib().moe_kv_gather(C.byref(cache), slots, n, dtype, k_out, v_out, stream))

@@ -1,0 +1,124 @@
+// Shared by the kernels of the paged 8-bit cache: what a plan holds, conversions between codes and numbers.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/moe_kv.h"
+
+namespace moe {
+namespace kv {
+
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+
+constexpr int SUB = 16;            // tokens of a 16 x 16 tile of codes
+constexpr int KT = 32;             // tokens of a step of the attention kernels: the rows of one matrix instruction
+constexpr int ROWS_FEW = 32;       // (token, query head of the group) rows of a block whose waves share out the cached tokens
+constexpr int ROWS_MANY = 128;     // ... and of one whose waves share out the rows
+constexpr int BLOCKS_FEW = 1024;   // blocks that the cached tokens of small requests are shared out to at most, beyond one a request
+constexpr int BLOCKS_MANY = 512;
+constexpr int MIN_KT_FEW = 8;      // steps of a block at least where a request is split
+constexpr int MIN_KT_MANY = 16;
+
+// One block's work, for each kv head: rows [tile * ROWS, ...) of a request against the cached tokens [kt0, kt1) * KT.
+struct __align__(16) Item {
+    int32_t req, row0, n_new, ctx;      // row0: first packed row of the request; ctx: position of its token
+    int32_t tile, kt0, kt1, part;       // part: which partial result, -1: the block holds all and writes the output
+};
+struct __align__(16) Join {
+    int32_t row0, n_new, tile, part0;
+    int32_t parts, pad[3];
+};
+// New tokens of one page.
+struct __align__(16) Segment {
+    int32_t row0, count, page_id, offset;
+    int32_t pos0, pad[3];
+};
+struct Header {
+    int32_t segments, few, many, joins_few, joins_many, pad[11];
+};
+
+// Where a plan's lists lie in its buffer, and how long they can get.
+struct Plan {
+    Header *head;
+    int32_t *positions;
+    Segment *segments;
+    Item *few, *many;
+    Join *joins_few, *joins_many;
+    int32_t max_segments, max_few, max_many, max_joins_few, max_joins_many, parts_few, parts_many;
+};
+
+__host__ __device__ inline int div_up(int a, int b) { return (a + b - 1) / b; }
+
+// a new float from its sixteen bits
+template <int DTYPE>
+__device__ __forceinline__ float from_bits(uint32_t b)
+{
+    if constexpr (DTYPE == MOE_KV_F16) return (float)__builtin_bit_cast(_Float16, (uint16_t)b);
+    else return __builtin_bit_cast(float, b << 16);
+}
+
+// nearest, ties to even; NaN stays NaN
+template <int DTYPE>
+__device__ __forceinline__ uint32_t to_bits(float x)
+{
+    if constexpr (DTYPE == MOE_KV_F16) return __builtin_bit_cast(uint16_t, (_Float16)x);
+    else return __builtin_bit_cast(uint16_t, (__bf16)x);
+}
+
+template <int DTYPE>
+__device__ __forceinline__ uint32_t pack2(float a, float b)
+{
+    return to_bits<DTYPE>(a) | (to_bits<DTYPE>(b) << 16);
+}
+
+template <int FMT>
+constexpr float largest_code() { return FMT == MOE_KV_E4M3 ? 448.f : 127.f; }
+
+// Eight codes as fp16 numbers, exact in both formats.
+template <int FMT>
+__device__ __forceinline__ v8h codes_to_half(uint32_t lo, uint32_t hi)
+{
+    union { v8h v; v2h p[4]; uint32_t u[4]; } r;
+    if constexpr (FMT == MOE_KV_E4M3) {
+        r.p[0] = __builtin_bit_cast(v2h, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false));
+        r.p[1] = __builtin_bit_cast(v2h, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true));
+        r.p[2] = __builtin_bit_cast(v2h, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false));
+        r.p[3] = __builtin_bit_cast(v2h, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true));
+    } else {
+        // code + 128 as the low bits of 1024 .. 1279, then 1152 off
+        const v2h bias = {(_Float16)1152.f, (_Float16)1152.f};
+        lo ^= 0x80808080u;
+        hi ^= 0x80808080u;
+        r.u[0] = __builtin_amdgcn_perm(0x64646464u, lo, 0x04010400u);
+        r.u[1] = __builtin_amdgcn_perm(0x64646464u, lo, 0x04030402u);
+        r.u[2] = __builtin_amdgcn_perm(0x64646464u, hi, 0x04010400u);
+        r.u[3] = __builtin_amdgcn_perm(0x64646464u, hi, 0x04030402u);
+        for (int i = 0; i < 4; ++i) r.p[i] = r.p[i] - bias;
+    }
+    return r.v;
+}
+
+template <int FMT>
+__device__ __forceinline__ float code_to_float(uint32_t byte)
+{
+    if constexpr (FMT == MOE_KV_E4M3) return __builtin_amdgcn_cvt_f32_fp8((int)byte, 0);
+    else return (float)(int8_t)byte;
+}
+
+// Four numbers within the largest code (or NaN: 0) as codes, nearest, ties to even.
+template <int FMT>
+__device__ __forceinline__ uint32_t floats_to_codes(float a, float b, float c, float d)
+{
+    if constexpr (FMT == MOE_KV_E4M3) {
+        int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
+    } else {
+        const int i = (int)rintf(a), j = (int)rintf(b), k = (int)rintf(c), l = (int)rintf(d);
+        return (uint32_t)(i & 255) | ((uint32_t)(j & 255) << 8) | ((uint32_t)(k & 255) << 16) | ((uint32_t)l << 24);
+    }
+}
+
+}  // namespace kv
+}  // namespace moe

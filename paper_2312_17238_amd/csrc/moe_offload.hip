@@ -24,6 +24,7 @@
 
 #include "../../include/moe_offload.h"
 #include "cache.h"
+#include "errors.h"
 #include "kernels.h"
 #include "layout.h"
 
@@ -69,6 +70,12 @@ static int32_t on_exception(const char *what) noexcept
     } catch (...) {
         return fail(MOE_ESTATE, "%s: unknown exception", what);
     }
+}
+
+int32_t moe::report_error(int32_t code, int32_t hip_err, const char *text)
+{
+    if (hip_err) g_hip_err = hip_err;
+    return fail(code, "%s", text);
 }
 
 extern "C" const char *moe_last_error(void) { return g_err; }
