@@ -7,13 +7,13 @@
 // few rows, block 1 those of many, the others look up rows and pages with a binary search in the sums.  Latency is all there is
 // to it: 2048 requests with 77 thousand rows move 0.7 MB.
 #pragma once
+#include "kernels_common.h"
 #include "kernels_kv_common.h"
 
 namespace moe {
 namespace kv {
 
-constexpr int PLAN_THREADS = 1024;
-constexpr int PLAN_PER = MOE_KV_MAX_REQUESTS / PLAN_THREADS;   // requests of a thread at most
+constexpr int PLAN_MOST_THREADS = 1024;
 
 struct PlanArgs {
     moe_kv_step_t s;
@@ -22,31 +22,58 @@ struct PlanArgs {
     int32_t group, page_shift, target_few, target_many;
 };
 
-__device__ __forceinline__ int64_t wave_scan(int64_t v)
+// a + b, 2^32 - 1 at most: sums of lengths that no batch can have stay above every bound they are compared with
+__device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_or_0(uint32_t v)
 {
-    const int lane = threadIdx.x & 63;
-    for (int d = 1; d < 64; d *= 2) {
-        const int64_t o = __shfl_up(v, d);
-        if (lane >= d) v += o;
-    }
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+}
+
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v)
+{
+    v = add_sat(v, dpp_or_0<0x111, 0xf>(v));    // row_shr 1, 2, 4, 8: sums within sixteen lanes
+    v = add_sat(v, dpp_or_0<0x112, 0xf>(v));
+    v = add_sat(v, dpp_or_0<0x114, 0xf>(v));
+    v = add_sat(v, dpp_or_0<0x118, 0xf>(v));
+    v = add_sat(v, dpp_or_0<0x142, 0xa>(v));    // row_bcast 15 into rows 1 and 3, 31 into rows 2 and 3
+    v = add_sat(v, dpp_or_0<0x143, 0xc>(v));
     return v;
 }
 
-// Inclusive sum over the block's threads in their order; *total receives the whole sum.  `tmp`: 17 numbers in LDS.
-__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t *tmp, int64_t *total)
+// Inclusive sum over the block's threads in their order; *total receives the whole sum.  `tmp`: a number a wave, in LDS.
+template <int THREADS>
+__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t *tmp, uint32_t *total)
 {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     v = wave_scan(v);
-    __syncthreads();          // the last scan's readers are done with tmp
-    if (lane == 63) tmp[wave] = v;
-    __syncthreads();
-    int64_t before = 0, all = 0;
-    for (int w = 0; w < PLAN_THREADS / 64; ++w) {
-        if (w < wave) before += tmp[w];
-        all += tmp[w];
+    if constexpr (THREADS == 64) {
+        *total = (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+        return v;
+    } else {
+        __syncthreads();          // the last scan's readers are done with tmp
+        if (lane == 63) tmp[wave] = v;
+        __syncthreads();
+        const uint32_t sums = wave_scan(lane < THREADS / 64 ? tmp[lane] : 0);
+        *total = (uint32_t)__builtin_amdgcn_readlane((int)sums, 63);
+        return add_sat(v, wave ? (uint32_t)__shfl((int)sums, wave - 1) : 0);
     }
-    *total = all;
-    return v + before;
+}
+
+// Sum of whole numbers below 2^53 in all, in every thread.
+template <int THREADS>
+__device__ __forceinline__ double block_sum(double v, double *tmp)
+{
+    v = wave_sum_f64(v);
+    if constexpr (THREADS > 64) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = v;
+        __syncthreads();
+        const int lane = threadIdx.x & 63;
+        v = wave_sum_f64(lane < THREADS / 64 ? tmp[lane] : 0.0);
+    }
+    return v;
 }
 
 // first i with sums[i] > x, sums ascending; n if there is none
@@ -61,7 +88,7 @@ __device__ __forceinline__ int first_above(const int32_t *sums, int n, int x)
     return lo;
 }
 
-// Steps [kt0, kt1) over the cached tokens that rows [first, last] of a request see.
+// Steps [kt0, kt1) over the cached tokens that rows of a request see, tokens [tok_first, tok_last].
 __device__ __forceinline__ void key_steps(const moe_kv_step_t &s, int ctx, int n_new, int tok_first, int tok_last, int &kt0, int &kt1)
 {
     const int hi = s.causal ? ctx + tok_last + 1 : ctx + n_new;
@@ -70,21 +97,44 @@ __device__ __forceinline__ void key_steps(const moe_kv_step_t &s, int ctx, int n
     kt1 = (hi + KT - 1) / KT;
 }
 
-__global__ void __launch_bounds__(PLAN_THREADS) k_kv_plan(PlanArgs a)
+// The steps of a block where `all` steps are shared out to `target` blocks of at least `least`.
+__device__ __forceinline__ int share(double all, int target, int least)
+{
+    return max(least, (int)(((int64_t)all + target - 1) / target));
+}
+
+// Writes the items of one unit of work, in as many parts as `n`, and what joins them.
+__device__ __forceinline__ void put_items(Item *items, Join *joins, Item it, int n, int item0, int join0, int part0)
+{
+    const int lo = it.kt0, len = it.kt1 - it.kt0;
+    if (n > 1) joins[join0] = Join{it.row0, it.n_new, it.tile, part0, n, {0, 0, 0}};
+    for (int p = 0; p < n; ++p) {
+        it.kt0 = lo + (int)((int64_t)len * p / n);
+        it.kt1 = lo + (int)((int64_t)len * (p + 1) / n);
+        it.part = n > 1 ? part0 + p : -1;
+        items[item0 + p] = it;
+    }
+}
+
+// THREADS: a thread has at most PER requests.  64 threads, whose sums need no LDS and no barrier, are MEASURED_PLAN.
+template <int THREADS, int PER>
+__global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
 {
     extern __shared__ int32_t lds[];
-    __shared__ int64_t tmp[PLAN_THREADS / 64];
+    __shared__ double tmp_d[THREADS / 64];
+    uint32_t *tmp = reinterpret_cast<uint32_t *>(tmp_d);
     const moe_kv_step_t &s = a.s;
-    const int R = s.n_requests, T = s.n_tokens, tid = threadIdx.x, page = s.page;
+    const int R = s.n_requests, T = s.n_tokens, tid = threadIdx.x, page = s.page, shift = a.page_shift;
     int32_t *row_end = lds, *need_before = lds + R, *sums = lds + 2 * R;   // sums: what the block's own role needs
-    const int per = div_up(R, PLAN_THREADS), r0 = tid * per;
+    const int per = PER == 1 ? 1 : div_up(R, THREADS), r0 = tid * per;
     const int free_n = min(max(0, a.io.free_count[0]), s.n_pages);
+    auto pages = [&](int n) { return (int)(((uint32_t)n + page - 1) >> shift); };      // n < 2^31
 
     // rows
-    int ctx[PLAN_PER], now[PLAN_PER], st[PLAN_PER];
-    int64_t sum = 0, total;
+    int ctx[PER], now[PER], st[PER], first[PER];
+    uint32_t sum = 0, total;
 #pragma unroll
-    for (int i = 0; i < PLAN_PER; ++i) {
+    for (int i = 0; i < PER; ++i) {
         const int r = r0 + i;
         ctx[i] = now[i] = st[i] = 0;
         if (i < per && r < R) {
@@ -94,174 +144,191 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_kv_plan(PlanArgs a)
             ctx[i] = max(ctx[i], 0);
             now[i] = min(max(now[i], 0), T + 1);
         }
-        sum += now[i];
+        sum = add_sat(sum, now[i]);
     }
-    int64_t at = block_scan(sum, tmp, &total) - sum;
+    uint32_t at = block_scan<THREADS>(sum, tmp, &total) - sum;
     // pages needed
-    int64_t need_sum = 0;
-    int need[PLAN_PER];
+    uint32_t need_sum = 0;
+    int need[PER];
 #pragma unroll
-    for (int i = 0; i < PLAN_PER; ++i) {
+    for (int i = 0; i < PER; ++i) {
         const int r = r0 + i;
-        const int64_t first = at;
-        at += now[i];
+        first[i] = (int)min(at, (uint32_t)T);
+        at = add_sat(at, now[i]);
         need[i] = 0;
         if (i < per && r < R) {
-            if (at > T) st[i] = MOE_KV_BAD_SIZE;
-            const int64_t blocks = ((int64_t)ctx[i] + now[i] + page - 1) >> a.page_shift;
+            if (at > (uint32_t)T) st[i] = MOE_KV_BAD_SIZE;
+            const int blocks = (int)(((uint32_t)ctx[i] + (uint32_t)now[i] + page - 1) >> shift);    // below 2^31 + 2^20 tokens
             if (!st[i] && blocks > s.max_blocks) st[i] = MOE_KV_TOO_LONG;
-            if (!st[i]) need[i] = (int)(blocks - (((int64_t)ctx[i] + page - 1) >> a.page_shift));
-            row_end[r] = (int)min(at, (int64_t)T);
-            now[i] = (int)(min(at, (int64_t)T) - min(first, (int64_t)T));     // rows that exist
+            if (!st[i]) need[i] = blocks - pages(ctx[i]);
+            const int end = (int)min(at, (uint32_t)T);
+            row_end[r] = end;
+            now[i] = end - first[i];                        // rows that exist
         }
-        need_sum += need[i];
+        need_sum = add_sat(need_sum, need[i]);
     }
-    int64_t before = block_scan(need_sum, tmp, &total) - need_sum;
-    int64_t used = 0;
+    uint32_t before = block_scan<THREADS>(need_sum, tmp, &total) - need_sum;
+    uint32_t used = 0;
 #pragma unroll
-    for (int i = 0; i < PLAN_PER; ++i) {
+    for (int i = 0; i < PER; ++i) {
         const int r = r0 + i;
         if (i < per && r < R) {
-            if (need[i] > 0 && before + need[i] > free_n) st[i] = MOE_KV_NO_PAGES;
+            if (need[i] > 0 && add_sat(before, need[i]) > (uint32_t)free_n) st[i] = MOE_KV_NO_PAGES;
             if (!st[i]) used += need[i];
-            need_before[r] = st[i] ? -1 : (int)before;      // at most free_n where it is used
+            need_before[r] = st[i] ? -1 : (int)min(before, 0x7FFFFFFFu);      // at most free_n where it is used
         }
-        before += need[i];
+        before = add_sat(before, need[i]);
     }
 
     const int role = blockIdx.x;
     if (role == 0) {
-        block_scan(used, tmp, &total);
+        // what is per request, and the requests of few rows
+        block_scan<THREADS>(used, tmp, &total);
+        Item it[PER];
+        double steps = 0.0;
 #pragma unroll
-        for (int i = 0; i < PLAN_PER; ++i) {
-            const int r = r0 + i;
+        for (int i = 0; i < PER; ++i) {
+            const int r = r0 + i, rows = now[i] * a.group;
+            it[i] = Item{r, first[i], rows == 0 || rows > ROWS_FEW || st[i] == MOE_KV_BAD_SIZE ? 0 : now[i], ctx[i], 0, 0, 0, -1};
             if (i < per && r < R) {
-                a.io.row_start[r + 1] = row_end[r];
+                a.io.row_start[r + 1] = first[i] + now[i];
                 a.io.kv_len[r] = st[i] ? ctx[i] : ctx[i] + now[i];
                 a.io.status[r] = st[i];
+                if (it[i].n_new && !st[i]) key_steps(s, ctx[i], now[i], 0, now[i] - 1, it[i].kt0, it[i].kt1);
             }
+            steps += it[i].kt1 - it[i].kt0;
         }
         if (tid == 0) {
             a.io.row_start[0] = 0;
-            a.io.free_left[0] = (int)(free_n - total);
+            a.io.free_left[0] = free_n - (int)total;
         }
+        const int chunk = share(block_sum<THREADS>(steps, tmp_d), a.target_few, MIN_KT_FEW);
+        uint32_t items = 0, split = 0;                   // split: joins << 16 | parts
+        int n[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            n[i] = it[i].n_new ? max(1, div_up(it[i].kt1 - it[i].kt0, chunk)) : 0;
+            items += n[i];
+            split += n[i] > 1 ? (1u << 16) + n[i] : 0;
+        }
+        uint32_t all_items, all_split;
+        uint32_t item0 = block_scan<THREADS>(items, tmp, &all_items) - items, split0 = block_scan<THREADS>(split, tmp, &all_split) - split;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            put_items(a.p.few, a.p.joins_few, it[i], n[i], item0, split0 >> 16, split0 & 0xFFFF);
+            item0 += n[i];
+            split0 += n[i] > 1 ? (1u << 16) + n[i] : 0;
+        }
+        if (tid == 0) {
+            a.p.head->few = (int)all_items;
+            a.p.head->joins_few = (int)(all_split >> 16);
+        }
+        return;
     }
-    if (role <= 1) {
-        // Units: requests of few rows (block 0), tiles of 128 rows of the others (block 1).  A request of a bad size
-        // has none: it may have more rows than the lists are made for.
-        const bool many = role == 1;
-        auto units_of = [&](int i) {
-            const int rows = st[i] == MOE_KV_BAD_SIZE ? 0 : now[i] * a.group;
-            return rows == 0 || (rows > ROWS_FEW) != many ? 0 : many ? div_up(rows, ROWS_MANY) : 1;
+    if (role == 1) {
+        // Tiles of 128 rows of the other requests.  A request of a bad size has none: it may have more rows than the lists
+        // are made for.
+        auto tiles_of = [&](int i) {
+            const int rows = now[i] * a.group;
+            return rows <= ROWS_FEW || st[i] == MOE_KV_BAD_SIZE ? 0 : div_up(rows, ROWS_MANY);
         };
-        int64_t units = 0;
+        uint32_t units = 0, n_units;
 #pragma unroll
-        for (int i = 0; i < PLAN_PER; ++i) {
-            units += units_of(i);
+        for (int i = 0; i < PER; ++i) units += tiles_of(i);
+        uint32_t unit_at = block_scan<THREADS>(units, tmp, &n_units) - units;
+        if (n_units == 0) {
+            if (tid == 0) a.p.head->many = a.p.head->joins_many = 0;
+            return;
         }
-        int64_t n_units;
-        int64_t unit_at = block_scan(units, tmp, &n_units) - units;
 #pragma unroll
-        for (int i = 0; i < PLAN_PER; ++i) {
-            const int r = r0 + i;
-            unit_at += units_of(i);
-            if (i < per && r < R) sums[r] = (int)unit_at;
+        for (int i = 0; i < PER; ++i) {
+            unit_at += tiles_of(i);
+            if (i < per && r0 + i < R) sums[r0 + i] = (int)unit_at;
         }
         __syncthreads();
-        const int tile_rows = many ? ROWS_MANY : ROWS_FEW;
         auto unit = [&](int u, Item &it) {
             const int r = first_above(sums, R, u);
             const int begin = r ? row_end[r - 1] : 0, n = row_end[r] - begin;
-            const int local = u - (r ? sums[r - 1] : 0), tiles = sums[r] - (r ? sums[r - 1] : 0);
             it.req = r;
             it.row0 = begin;
             it.n_new = n;
             it.ctx = max(a.io.ctx_len[r], 0);
-            it.tile = tiles - 1 - local;                 // the last rows see most: they go first
+            it.tile = sums[r] - 1 - u;                   // the last rows see most: they go first
             it.kt0 = it.kt1 = 0;                         // turned down: nothing to attend to
             if (need_before[r] >= 0)
-                key_steps(s, it.ctx, n, it.tile * tile_rows / a.group, (min((it.tile + 1) * tile_rows, n * a.group) - 1) / a.group, it.kt0, it.kt1);
+                key_steps(s, it.ctx, n, it.tile * ROWS_MANY / a.group, (min((it.tile + 1) * ROWS_MANY, n * a.group) - 1) / a.group, it.kt0, it.kt1);
         };
-        int64_t steps = 0, all_steps;
-        for (int u = tid; u < n_units; u += PLAN_THREADS) {
+        double steps = 0.0;
+        for (int u = tid; u < (int)n_units; u += THREADS) {
             Item it{};
             unit(u, it);
             steps += it.kt1 - it.kt0;
         }
-        block_scan(steps, tmp, &all_steps);
-        const int target = many ? a.target_many : a.target_few;
-        const int chunk = (int)max((int64_t)(many ? MIN_KT_MANY : MIN_KT_FEW), (all_steps + target - 1) / target);
-        int64_t done = 0;                                // items | joins << 24 | parts << 44, so far
-        for (int base = 0; base < n_units; base += PLAN_THREADS) {
+        const int chunk = share(block_sum<THREADS>(steps, tmp_d), a.target_many, MIN_KT_MANY);
+        uint32_t items = 0, split = 0;
+        for (int base = 0; base < (int)n_units; base += THREADS) {
             Item it{};
             int n = 0;
-            if (base + tid < n_units) {
+            if (base + tid < (int)n_units) {
                 unit(base + tid, it);
                 n = max(1, div_up(it.kt1 - it.kt0, chunk));
             }
-            const int64_t mine = n | (n > 1 ? ((int64_t)1 << 24) | ((int64_t)n << 44) : 0);
-            int64_t all;
-            const int64_t upto = done + block_scan(mine, tmp, &all) - mine;
-            done += all;
-            const int item0 = (int)(upto & 0xFFFFFF), join0 = (int)((upto >> 24) & 0xFFFFF), part0 = (int)(upto >> 44);
-            const int lo = it.kt0, len = it.kt1 - it.kt0;
-            for (int p = 0; p < n; ++p) {
-                it.kt0 = lo + (int)((int64_t)len * p / n);
-                it.kt1 = lo + (int)((int64_t)len * (p + 1) / n);
-                it.part = n > 1 ? part0 + p : -1;
-                (many ? a.p.many : a.p.few)[item0 + p] = it;
-            }
-            if (n > 1) (many ? a.p.joins_many : a.p.joins_few)[join0] = Join{it.row0, it.n_new, it.tile, part0, n, {0, 0, 0}};
+            const uint32_t mine = n > 1 ? (1u << 16) + n : 0;
+            uint32_t all_items, all_split;
+            const uint32_t item0 = items + block_scan<THREADS>(n, tmp, &all_items) - n, split0 = split + block_scan<THREADS>(mine, tmp, &all_split) - mine;
+            items += all_items;
+            split += all_split;
+            put_items(a.p.many, a.p.joins_many, it, n, item0, split0 >> 16, split0 & 0xFFFF);
         }
         if (tid == 0) {
-            (many ? a.p.head->many : a.p.head->few) = (int)(done & 0xFFFFFF);
-            (many ? a.p.head->joins_many : a.p.head->joins_few) = (int)((done >> 24) & 0xFFFFF);
+            a.p.head->many = (int)items;
+            a.p.head->joins_many = (int)(split >> 16);
         }
         return;
     }
 
     // pages touched
-    int64_t touched = 0, n_seg;
-    int seg[PLAN_PER];
+    uint32_t touched = 0, n_seg;
+    int seg[PER];
 #pragma unroll
-    for (int i = 0; i < PLAN_PER; ++i) {
-        seg[i] = st[i] || !now[i] ? 0 : (int)((((int64_t)ctx[i] + now[i] + page - 1) >> a.page_shift) - (ctx[i] >> a.page_shift));
+    for (int i = 0; i < PER; ++i) {
+        seg[i] = st[i] || !now[i] ? 0 : pages(ctx[i] + now[i]) - (ctx[i] >> shift);
         touched += seg[i];
     }
-    int64_t seg_at = block_scan(touched, tmp, &n_seg) - touched;
+    uint32_t seg_at = block_scan<THREADS>(touched, tmp, &n_seg) - touched;
 #pragma unroll
-    for (int i = 0; i < PLAN_PER; ++i) {
+    for (int i = 0; i < PER; ++i) {
         seg_at += seg[i];
         if (i < per && r0 + i < R) sums[r0 + i] = (int)seg_at;
     }
     __syncthreads();
     // A page of a request: an old one from the table, a new one from the stack.
     auto page_of = [&](int r, int c, int blk) {
-        const int held = (int)(((int64_t)c + page - 1) >> a.page_shift);
+        const int held = pages(c);
         if (blk < held) return a.io.block_table[(int64_t)r * s.max_blocks + blk];
         return a.io.free_pages[free_n - 1 - (need_before[r] + blk - held)];
     };
     const int worker = role - 2, workers = gridDim.x - 2;
-    for (int t = worker * PLAN_THREADS + tid; t < T; t += workers * PLAN_THREADS) {
+    for (int t = worker * THREADS + tid; t < T; t += workers * THREADS) {
         const int r = first_above(row_end, R, t);
         int pos = -1, slot = -1;
         if (r < R && need_before[r] >= 0) {
             const int c = max(a.io.ctx_len[r], 0);
             pos = c + t - (r ? row_end[r - 1] : 0);
-            const int id = page_of(r, c, pos >> a.page_shift);
+            const int id = page_of(r, c, pos >> shift);
             if ((unsigned)id < (unsigned)s.n_pages) slot = id * page + (pos & (page - 1));
         }
         a.io.positions[t] = pos;
         a.p.positions[t] = pos;
         a.io.slots[t] = slot;
     }
-    for (int g = worker * PLAN_THREADS + tid; g < n_seg; g += workers * PLAN_THREADS) {
+    for (int g = worker * THREADS + tid; g < (int)n_seg; g += workers * THREADS) {
         const int r = first_above(sums, R, g);
         const int c = max(a.io.ctx_len[r], 0), begin = r ? row_end[r - 1] : 0, n = row_end[r] - begin;
-        const int blk = (c >> a.page_shift) + g - (r ? sums[r - 1] : 0);
-        const int lo = max(c, blk << a.page_shift), hi = min(c + n, (blk + 1) << a.page_shift);
+        const int blk = (c >> shift) + g - (r ? sums[r - 1] : 0);
+        const int lo = max(c, blk << shift), hi = min(c + n, (blk + 1) << shift);
         const int id = page_of(r, c, blk);
-        if ((int64_t)blk << a.page_shift >= c) a.io.block_table[(int64_t)r * s.max_blocks + blk] = id;
+        if (blk << shift >= c) a.io.block_table[(int64_t)r * s.max_blocks + blk] = id;
         a.p.segments[g] = Segment{begin + lo - c, hi - lo, (unsigned)id < (unsigned)s.n_pages ? id : -1, lo & (page - 1), lo, {0, 0, 0}};
     }
     if (worker == 0 && tid == 0) a.p.head->segments = (int)n_seg;

@@ -152,8 +152,13 @@ extern "C" int32_t moe_kv_plan(const moe_kv_step_t *step, const moe_kv_lists_t *
     }
     const Sizes z = sizes_of(step);
     PlanArgs a{*step, *io, plan_at(z, plan_dev), z.group, log2_of(step->page), target_blocks(BLOCKS_FEW, step->kv_heads), target_blocks(BLOCKS_MANY, step->kv_heads)};
-    const int workers = std::min(254, div_up(std::max(step->n_tokens, z.p.max_segments), PLAN_THREADS));
-    hipLaunchKernelGGL(k_kv_plan, dim3(2 + workers), dim3(PLAN_THREADS), (size_t)step->n_requests * 12, static_cast<hipStream_t>(stream), a);
+    const int R = step->n_requests, threads = R <= 64 ? 64 : R <= 256 ? 256 : PLAN_MOST_THREADS;
+    const dim3 grid(2 + std::min(254, div_up(std::max(step->n_tokens, z.p.max_segments), threads)));
+    const size_t lds = (size_t)R * 12;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (threads == 64) hipLaunchKernelGGL((k_kv_plan<64, 1>), grid, dim3(64), lds, st, a);
+    else if (threads == 256) hipLaunchKernelGGL((k_kv_plan<256, 1>), grid, dim3(256), lds, st, a);
+    else hipLaunchKernelGGL((k_kv_plan<PLAN_MOST_THREADS, MOE_KV_MAX_REQUESTS / PLAN_MOST_THREADS>), grid, dim3(PLAN_MOST_THREADS), lds, st, a);
     return launched("moe_kv_plan");
 }
 

@@ -11,6 +11,7 @@ Everything runs on torch's current stream and reads no length on the host.  All 
 """
 from __future__ import annotations
 
+import ctypes as C
 import math
 from typing import Optional, Tuple
 
@@ -21,9 +22,12 @@ from . import binding as B
 DTYPES = {torch.float16: B.MOE_KV_F16, torch.bfloat16: B.MOE_KV_BF16}
 FORMATS = {torch.float8_e4m3fn: B.MOE_KV_E4M3, torch.int8: B.MOE_KV_INT8}
 
+# A call costs the host a few microseconds, which for single tokens is what counts: structures and references to them are made once,
+# messages only when something is refused.
+
 
 def _stream(t: torch.Tensor) -> int:
-    return torch.cuda.current_stream(t.device).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(t.device.index)
 
 
 def _need(ok: bool, what: str) -> None:
@@ -32,17 +36,20 @@ def _need(ok: bool, what: str) -> None:
 
 
 def _ints(t: torch.Tensor, shape, what: str) -> int:
-    _need(t.dtype == torch.int32 and t.is_cuda and t.is_contiguous() and tuple(t.shape) == tuple(shape),
-          f"{what}: a contiguous int32 tensor {tuple(shape)} on the GPU is needed, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.dtype is not torch.int32 or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous int32 tensor {tuple(shape)} on the GPU is needed, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _rows(t: torch.Tensor, n: int, heads: int, dim: int, dtype, what: str) -> Tuple[int, int]:
+def _rows(t: torch.Tensor, shape, dtype, what: str) -> Tuple[int, int]:
     """(pointer, elements between rows) of [n][heads][dim] whose heads follow each other."""
-    _need(t.dtype == dtype and t.is_cuda, f"{what}: {t.dtype} on {t.device}, {dtype} on the GPU is needed")
-    _need(tuple(t.shape) == (n, heads, dim), f"{what}: shape {tuple(t.shape)}, ({n}, {heads}, {dim}) is needed")
-    _need(t.stride(2) == 1 and (heads == 1 or t.stride(1) == dim), f"{what}: the heads of a row have to follow each other")
-    return t.data_ptr(), t.stride(0) if n > 1 else heads * dim
+    n, heads, dim = shape
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda:
+        raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)} on {t.device}, {dtype} {shape} on the GPU is needed")
+    row, head, one = t.stride()
+    if one != 1 or (head != dim and heads != 1):
+        raise ValueError(f"{what}: the heads of a row have to follow each other")
+    return t.data_ptr(), row if n > 1 else heads * dim
 
 
 class Cache:
@@ -62,6 +69,7 @@ class Cache:
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_pages, self.kv_heads, self.page, self.head_dim = p, h, 16 * s, 16 * d
         self.c = B.KvCache(p, 16 * s, h, 16 * d, FORMATS[k.dtype], 0, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+        self.ref = C.byref(self.c)
 
     @classmethod
     def empty(cls, n_pages: int, kv_heads: int, head_dim: int, page: int = 64, dtype=torch.float8_e4m3fn, device="cuda:0") -> "Cache":
@@ -88,19 +96,25 @@ class Step:
         self.kv_len, self.status, self.free_left = i32(n_requests), i32(n_requests), i32(1)
         self.plan_dev = torch.empty(n, dtype=torch.uint8, device=device)
         self.scratch_bytes = B.moe_kv_scratch_bytes(self.s)
-        self._scratch: Optional[torch.Tensor] = None
+        self.scratch = torch.empty(max(16, self.scratch_bytes), dtype=torch.uint8, device=device)
         self.block_table: Optional[torch.Tensor] = None
+        self._lists = B.KvLists(*[None] * 5, *(t.data_ptr() for t in (self.row_start, self.positions, self.slots, self.kv_len, self.status, self.free_left)))
+        self._row, self._query = B.KvRows(), B.KvQuery()
+        self._ref, self._lists_ref, self._row_ref, self._query_ref = (C.byref(x) for x in (self.s, self._lists, self._row, self._query))
+        self._per_request, self._table = (n_requests,), (n_requests, max_blocks)
+        self._q_shape, self._kv_shape = (n_tokens, q_heads, head_dim), (n_tokens, kv_heads, head_dim)
+        self._scale = 1.0 / math.sqrt(head_dim)
 
     def plan(self, ctx_len, new_len, block_table, free_pages, free_count) -> None:
         """Pages for the step's new tokens (block_table is updated in place, ctx_len and the stack stay until `advance`)."""
-        s = self.s
+        x = self._lists
+        x.ctx_len, x.new_len = _ints(ctx_len, self._per_request, "ctx_len"), _ints(new_len, self._per_request, "new_len")
+        x.block_table = _ints(block_table, self._table, "block_table")
         _need(free_pages.dim() == 1 and free_pages.numel() >= 1, "plan: free_pages is a list")
-        lists = B.KvLists(_ints(ctx_len, (s.n_requests,), "ctx_len"), _ints(new_len, (s.n_requests,), "new_len"),
-                          _ints(block_table, (s.n_requests, s.max_blocks), "block_table"),
-                          _ints(free_pages, free_pages.shape, "free_pages"), _ints(free_count, (1,), "free_count"),
-                          self.row_start.data_ptr(), self.positions.data_ptr(), self.slots.data_ptr(),
-                          self.kv_len.data_ptr(), self.status.data_ptr(), self.free_left.data_ptr())
-        B.moe_kv_plan(s, lists, self.plan_dev.data_ptr(), _stream(self.plan_dev))
+        x.free_pages, x.free_count = _ints(free_pages, free_pages.shape, "free_pages"), _ints(free_count, (1,), "free_count")
+        rc = B.lib().moe_kv_plan(self._ref, self._lists_ref, self.plan_dev.data_ptr(), _stream(self.plan_dev))
+        if rc:
+            B.check(rc)
         self.block_table, self._ctx, self._count = block_table, ctx_len, free_count
 
     def advance(self) -> None:
@@ -109,15 +123,6 @@ class Step:
         self._ctx.copy_(self.kv_len)
         self._count.copy_(self.free_left)
 
-    def scratch(self) -> torch.Tensor:
-        if self._scratch is None:
-            self._scratch = torch.empty(max(16, self.scratch_bytes), dtype=torch.uint8, device=self.plan_dev.device)
-        return self._scratch
-
-
-def _on(step: Step, what: str) -> None:
-    _need(step.block_table is not None, f"{what}: the step has no plan yet")
-
 
 def write(cache: Cache, step: Step, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_gamma: Optional[torch.Tensor] = None,
           k_gamma: Optional[torch.Tensor] = None, eps: float = 0.0, inv_freq: Optional[torch.Tensor] = None, interleaved: bool = False,
@@ -125,51 +130,70 @@ def write(cache: Cache, step: Step, q: torch.Tensor, k: torch.Tensor, v: torch.T
     """Norm (eps > 0) and rotation (inv_freq: fp32, one number a pair) of queries and keys; keys and values go into
     the cache.  q [n_tokens, q_heads, head_dim], k, v [n_tokens, kv_heads, head_dim], views of one packed tensor among them.
     Returns the queries: q_out (which may be q), a new tensor if it is None; rows that belong to no request are left as they are."""
-    _on(step, "write")
-    s = step.s
-    _need(q.dtype in DTYPES, f"write: queries of type {q.dtype}")
-    d, n = s.head_dim, s.n_tokens
+    _need(step.block_table is not None, "write: the step has no plan yet")
+    dtype, x = q.dtype, step._row
+    if dtype not in DTYPES:
+        raise ValueError(f"write: queries of type {dtype}")
     if q_out is None:
-        q_out = torch.empty(n, s.q_heads, d, dtype=q.dtype, device=q.device)
-    (qp, qs), (op, os_) = _rows(q, n, s.q_heads, d, q.dtype, "q"), _rows(q_out, n, s.q_heads, d, q.dtype, "q_out")
-    (kp, ks), (vp, vs) = _rows(k, n, s.kv_heads, d, q.dtype, "k"), _rows(v, n, s.kv_heads, d, q.dtype, "v")
-    for g, what in ((q_gamma, "q_gamma"), (k_gamma, "k_gamma")):
-        _need(g is None or (tuple(g.shape) == (d,) and g.dtype == q.dtype and g.is_contiguous() and g.device == q.device), f"write: {what}: {d} contiguous numbers of type {q.dtype} are needed")
-        _need(g is None or eps > 0, f"write: {what} without a norm (eps is 0)")
-    rot = 0
-    if inv_freq is not None:
-        _need(inv_freq.dtype == torch.float32 and inv_freq.dim() == 1 and inv_freq.is_contiguous() and inv_freq.device == q.device, "write: inv_freq is a contiguous fp32 list")
-        rot = 2 * inv_freq.numel()
-    rows = B.KvRows(DTYPES[q.dtype], rot, int(interleaved), eps, qp, kp, vp, qs, ks, vs,
-                    q_gamma.data_ptr() if q_gamma is not None else None, k_gamma.data_ptr() if k_gamma is not None else None,
-                    inv_freq.data_ptr() if rot else None, op, os_)
-    B.moe_kv_write(cache.c, s, step.plan_dev.data_ptr(), rows, _stream(q))
+        q_out = torch.empty(step._q_shape, dtype=dtype, device=q.device)
+    x.q, x.q_stride = _rows(q, step._q_shape, dtype, "q")
+    x.q_out, x.q_out_stride = _rows(q_out, step._q_shape, dtype, "q_out")
+    x.k, x.k_stride = _rows(k, step._kv_shape, dtype, "k")
+    x.v, x.v_stride = _rows(v, step._kv_shape, dtype, "v")
+    x.dtype, x.eps, x.interleaved = DTYPES[dtype], eps, interleaved
+    x.q_gamma, x.k_gamma = _gain(q_gamma, step, eps, dtype, "q_gamma"), _gain(k_gamma, step, eps, dtype, "k_gamma")
+    x.rot_dim, x.inv_freq = 0, None
+    if inv_freq is not None and inv_freq.numel():
+        if inv_freq.dtype is not torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous() or not inv_freq.is_cuda:
+            raise ValueError("write: inv_freq is a contiguous fp32 list on the GPU")
+        x.rot_dim, x.inv_freq = 2 * inv_freq.numel(), inv_freq.data_ptr()
+    rc = B.lib().moe_kv_write(cache.ref, step._ref, step.plan_dev.data_ptr(), step._row_ref, _stream(q))
+    if rc:
+        B.check(rc)
     return q_out
+
+
+def _gain(g: Optional[torch.Tensor], step: Step, eps: float, dtype, what: str) -> Optional[int]:
+    if g is None:
+        return None
+    if g.shape != step._q_shape[2:] or g.dtype is not dtype or not g.is_contiguous() or not g.is_cuda:
+        raise ValueError(f"write: {what}: {step._q_shape[2]} contiguous numbers of type {dtype} are needed")
+    _need(eps > 0, "write: a gain without a norm (eps is 0)")
+    return g.data_ptr()
 
 
 def attend(cache: Cache, step: Step, q: torch.Tensor, scale: Optional[float] = None, out: Optional[torch.Tensor] = None, with_lse: bool = False):
     """Attention of the step's rows over all that is cached for their requests (scale: 1/sqrt(head_dim) if None).  Returns out [n_tokens,
     q_heads, head_dim], or (out, lse [n_tokens, q_heads] fp32); rows that belong to no request are left as they are."""
-    _on(step, "attend")
-    s = step.s
-    _need(q.dtype in DTYPES, f"attend: queries of type {q.dtype}")
+    table = step.block_table
+    _need(table is not None, "attend: the step has no plan yet")
+    dtype, x = q.dtype, step._query
+    if dtype not in DTYPES:
+        raise ValueError(f"attend: queries of type {dtype}")
     if out is None:
-        out = torch.empty(s.n_tokens, s.q_heads, s.head_dim, dtype=q.dtype, device=q.device)
-    (qp, qs), (op, os_) = _rows(q, s.n_tokens, s.q_heads, s.head_dim, q.dtype, "q"), _rows(out, s.n_tokens, s.q_heads, s.head_dim, q.dtype, "out")
-    lse = torch.empty(s.n_tokens, s.q_heads, dtype=torch.float32, device=q.device) if with_lse else None
-    query = B.KvQuery(DTYPES[q.dtype], 1.0 / math.sqrt(s.head_dim) if scale is None else scale, qp, qs, op, os_, lse.data_ptr() if with_lse else None)
-    B.moe_kv_attend(cache.c, s, step.plan_dev.data_ptr(), step.block_table.data_ptr(), query, step.scratch().data_ptr(), step.scratch_bytes, _stream(q))
+        out = torch.empty(step._q_shape, dtype=dtype, device=q.device)
+    lse = torch.empty(step._q_shape[:2], dtype=torch.float32, device=q.device) if with_lse else None
+    x.q, x.q_stride = _rows(q, step._q_shape, dtype, "q")
+    x.out, x.out_stride = _rows(out, step._q_shape, dtype, "out")
+    x.dtype, x.scale, x.lse = DTYPES[dtype], step._scale if scale is None else scale, lse.data_ptr() if with_lse else None
+    rc = B.lib().moe_kv_attend(cache.ref, step._ref, step.plan_dev.data_ptr(), table.data_ptr(), step._query_ref, step.scratch.data_ptr(),
+                               step.scratch_bytes, _stream(q))
+    if rc:
+        B.check(rc)
     return (out, lse) if with_lse else out
 
 
 def gather(cache: Cache, slots: torch.Tensor, dtype=torch.float16) -> Tuple[torch.Tensor, torch.Tensor]:
     """The keys and values that the tokens in `slots` stand for, [n, kv_heads, head_dim] each; zeros for a slot of -1."""
-    _need(dtype in DTYPES, f"gather: values of type {dtype}")
+    if dtype not in DTYPES:
+        raise ValueError(f"gather: values of type {dtype}")
     _need(slots.dim() == 1, "gather: slots is a list")
     p, n = _ints(slots, slots.shape, "slots"), slots.numel()
     k = torch.empty(n, cache.kv_heads, cache.head_dim, dtype=dtype, device=slots.device)
     v = torch.empty_like(k)
-    B.moe_kv_gather(cache.c, p, n, DTYPES[dtype], k.data_ptr(), v.data_ptr(), _stream(slots))
+    rc = B.lib().moe_kv_gather(cache.ref, p, n, DTYPES[dtype], k.data_ptr(), v.data_ptr(), _stream(slots))
+    if rc:
+        B.check(rc)
     return k, v
 
 

@@ -397,7 +397,7 @@ def test_attend(case):
     q = p.rows(sum(new) + 1, p.q_heads, spread=0.5)
     scale = 1 / math.sqrt(p.dim)
     out = torch.full_like(q, 7.0)
-    s._scratch, fence = fenced(max(16, s.scratch_bytes))
+    s.scratch, fence = fenced(max(16, s.scratch_bytes))
     out, lse = paged.attend(p.cache, s, q, scale, out=out, with_lse=True)
     assert (out[-1] == 7).all() and (fence == 0x5A).all()       # the last row is no request's
     check_attend(p, s, q, out, lse, lens, new, scale, rows=6)
@@ -516,7 +516,6 @@ def test_a_captured_step_serves_other_lengths():
     def make():
         p = Pool(3, 40, page=16, q_heads=4, kv_heads=2, fmt="int8", seed=5)
         s = paged.Step(3, 30, 20, 40, p.n_pages, 16, 4, 2, 64)
-        s.scratch()
         t = {"new": i32([0, 0, 0]), "x": torch.zeros(30, 8, 64, dtype=torch.float16, device=DEV), "out": torch.zeros(30, 4, 64, dtype=torch.float16, device=DEV),
              "q": torch.zeros(30, 4, 64, dtype=torch.float16, device=DEV)}
         return p, s, t
@@ -560,7 +559,6 @@ def test_calls_follow_the_current_stream():
     s = p.step(new)
     want_q = paged.write(p.cache, s, x[:, :4], x[:, 4:6], x[:, 6:])
     want = paged.attend(p.cache, s, want_q)
-    s.scratch()
     late = torch.empty_like(x)
     torch.cuda.synchronize()
     side = torch.cuda.Stream()
