@@ -20,7 +20,6 @@
 namespace moe {
 namespace kv {
 
-constexpr int ATTEND_THREADS = 256;
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
 struct AttendArgs {
@@ -31,19 +30,53 @@ struct AttendArgs {
     float *part_few, *part_many;    // [part][kv head][rows][D] outputs, then [part][kv head][rows] (m, l)
     int32_t group, max_blocks, causal, window;
     int32_t sub_shift;              // log2 of a page's sub-blocks
-    int32_t many_blocks;            // blocks of the grid that take tiles of 128 rows; the others take requests of few rows
+    float per_group;                // 1 / group
+    int32_t many_blocks;            // blocks of the grid that take tiles of requests of many rows; the others those of few
     int32_t vec_q, vec_out;
 };
+
+// An item, in scalar registers.
+__device__ __forceinline__ Item item_of(const uint4 (&u)[3])
+{
+    union { Item it; uint4 u[3]; int w[12]; } r;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) r.u[i] = u[i];
+#pragma unroll
+    for (int i = 0; i < 12; ++i) r.w[i] = __builtin_amdgcn_readfirstlane(r.w[i]);
+    return r.it;
+}
+
+// A row of an item: its token and query head of the group, counted from the first of the tile, at most 256 rows in all.
+struct Row {
+    int tok, g;
+    bool real;
+};
+
+__device__ __forceinline__ Row row_at(const AttendArgs &a, int first, int row, int rows)
+{
+    // first / group is the same for all lanes; what is added to it is small enough for fp32's product to be exact after rounding down
+    const int t0 = first / a.group, in = first - t0 * a.group + row - first;
+    const int t = (int)(((float)in + 0.5f) * a.per_group);
+    return {t0 + t, in - t * a.group, row < rows};
+}
+
+__device__ __forceinline__ Item item_at(const Item *p)
+{
+    uint4 u[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) u[i] = reinterpret_cast<const uint4 *>(p)[i];
+    return item_of(u);
+}
 
 // What a row sees: tokens [lo, hi).
 struct Sees {
     int lo, hi;
 };
 
-__device__ __forceinline__ Sees sees(const AttendArgs &a, const Item &it, int row, int rows)
+__device__ __forceinline__ Sees sees(const AttendArgs &a, const Item &it, const Row &row)
 {
-    if (row >= rows) return {0, 0};
-    const int pos = it.ctx + row / a.group;
+    if (!row.real) return {0, 0};
+    const int pos = it.ctx + row.tok;
     return {a.window > 0 ? max(0, pos + 1 - a.window) : 0, a.causal ? pos + 1 : it.ctx + it.n_new};
 }
 
@@ -70,11 +103,11 @@ __device__ __forceinline__ void clear(State<D> &s)
 // Queries of 32 rows as the second operand of the first product.  k-slot (step 2i + c, lane half h, j) stands for dim
 // 16 (2i + h) + 8 c + j, as the key tiles have it.  unit: what the scores have to be multiplied with.
 template <int DTYPE, int D>
-__device__ __forceinline__ void load_queries(const AttendArgs &a, const Item &it, int head, int row, int rows, v8h (&q)[D / 16], float &unit)
+__device__ __forceinline__ void load_queries(const AttendArgs &a, const Item &it, int head, const Row &row, v8h (&q)[D / 16], float &unit)
 {
     const int h = (threadIdx.x >> 5) & 1;
-    const bool real = row < rows;
-    const int tok = real ? row / a.group : 0, g = real ? row - tok * a.group : 0;
+    const bool real = row.real;
+    const int tok = real ? row.tok : 0, g = real ? row.g : 0;
     const uint16_t *src = static_cast<const uint16_t *>(a.q.q) + (it.row0 + tok) * a.q.q_stride + (int64_t)(head * a.group + g) * D;
     uint32_t w[D / 4];
     uint32_t top = 0;
@@ -130,6 +163,14 @@ __device__ __forceinline__ uint4 keep_bytes(uint4 v, int lo, int hi)
     return make_uint4(v.x & (uint32_t)a, v.y & (uint32_t)(a >> 32), v.z & (uint32_t)b, v.w & (uint32_t)(b >> 32));
 }
 
+// The larger of lane l's and lane l ^ 32's number, in both.
+__device__ __forceinline__ float max_halves(float x)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);      // the lower lanes' in both, the upper lanes' in both
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+
 // One step: 32 cached tokens against 32 rows.  k, v: the lane's pieces of the two tiles.  sc: scale log2(e) ks of the lane's
 // sub-block, lv: log2 vs, iv: 1 / vs.  edge: some row does not see some token of the step.
 template <int FMT, int D>
@@ -152,7 +193,7 @@ __device__ __forceinline__ void step(State<D> &s, const v8h (&q)[D / 16], const 
 #pragma unroll
     for (int i = 1; i < 16; ++i) top = fmaxf(top, z[i]);
     float t = fmaf(top, sc, lv);
-    t = fmaxf(t, __shfl_xor(t, 32));
+    t = max_halves(t);
     if (__any(t > s.m)) {
         const float m = fmaxf(s.m, t);
         const float f = m == -INFINITY ? 1.f : exp2f(s.m - m);
@@ -209,7 +250,19 @@ __device__ __forceinline__ Place place_of(const AttendArgs &a, const Item &it, i
     return p;
 }
 
-// Writes four neighbouring numbers of an output row.
+// Writes two or four neighbouring numbers of an output row.
+template <int DTYPE>
+__device__ __forceinline__ void store2(void *out, int64_t at, bool vec, float a, float b)
+{
+    uint16_t *p = static_cast<uint16_t *>(out) + at;
+    if (vec) {
+        *reinterpret_cast<uint32_t *>(p) = pack2<DTYPE>(a, b);
+    } else {
+        p[0] = (uint16_t)to_bits<DTYPE>(a);
+        p[1] = (uint16_t)to_bits<DTYPE>(b);
+    }
+}
+
 template <int DTYPE>
 __device__ __forceinline__ void store4(void *out, int64_t at, bool vec, float a, float b, float c, float d)
 {
@@ -224,26 +277,162 @@ __device__ __forceinline__ void store4(void *out, int64_t at, bool vec, float a,
     }
 }
 
-// ---- a request of few rows: every wave takes every fourth step of the block's, straight from memory into registers
+// ---- joining the parts of rows whose cached tokens several blocks share
+// Each block leaves its outputs (scaled by 2^-m) and (m, l) in the scratch; the one that finds all others of its tile and head done
+// puts them together, in the parts' order, so that the result does not depend on which one that is.  What crosses blocks goes
+// past the dies' caches: stores and loads of agent scope, a wait for the stores' acknowledgement before the count.  A fence of
+// that scope would write back a die's whole cache for each of a thousand blocks; a second launch instead costs 4 to 10 us
+// on the GPU and 3.5 us of the host's time a layer.
+__device__ __forceinline__ void put2(float *p, float x, float y)
+{
+    const uint64_t w = __builtin_bit_cast(uint32_t, x) | ((uint64_t)__builtin_bit_cast(uint32_t, y) << 32);
+    __hip_atomic_store(reinterpret_cast<uint64_t *>(p), w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// (the address of all lanes, a lane's own bytes from there)
+__device__ __forceinline__ float get1(const float *p, uint32_t at)
+{
+    return __hip_atomic_load(reinterpret_cast<const float *>(reinterpret_cast<const char *>(p) + at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+__device__ __forceinline__ float2 get2(const float *p, uint32_t at)
+{
+    const uint64_t w = __hip_atomic_load(reinterpret_cast<const uint64_t *>(reinterpret_cast<const char *>(p) + at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__builtin_bit_cast(float, (uint32_t)w), __builtin_bit_cast(float, (uint32_t)(w >> 32)));
+}
+
+struct JoinShared {
+    float m[256], l[256];           // of a row
+    float4 sum[512];                // of a thread
+    int last;
+};
+
+// Counts this block's part; true in the block that came last.  Every thread's stores are acknowledged before the count.
+__device__ __forceinline__ bool all_parts_done(int32_t *count, int parts, JoinShared &sh)
+{
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        sh.last = __hip_atomic_fetch_add(count, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
+        if (sh.last) __hip_atomic_store(count, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);     // for the next layer
+    }
+    __syncthreads();
+    return sh.last;
+}
+
+// o: outputs [part][kv head][tile_rows][D], ml: [part][kv head][tile_rows][2]
+template <int DTYPE, int D>
+__device__ __forceinline__ void join_parts(const AttendArgs &a, const Item &it, int head, const float *o, const float *ml, int tile_rows, JoinShared &sh)
+{
+    constexpr int THREADS = 64 * attend_waves(D);
+    const int tid = threadIdx.x, heads = a.c.kv_heads;
+    const int rows = min(tile_rows, it.n_new * a.group - it.tile * tile_rows);
+    int pow2 = 4;
+    while (pow2 < rows) pow2 *= 2;
+    // 32 bits: about 1024 parts of all heads (see target_blocks), of at most 128 rows and 256 dims
+    auto at = [&](int p, int r) { return (uint32_t)(((it.part0 + p) * heads + head) * tile_rows + r); };
+    // Four dims a thread; where that leaves threads over, the parts are dealt out to groups of threads.  The loads are past the
+    // caches, one or two microseconds each: the first parts' are on their way before the maxima are known.
+    constexpr int QUADS = D / 4, AHEAD = D == 64 ? 8 : 16;
+    const int all = pow2 * QUADS, groups = max(1, THREADS / all);
+    const int e_first = groups > 1 ? tid % all : tid, g = groups > 1 ? tid / all : 0;
+    float m[AHEAD];
+    float2 x[AHEAD], y[AHEAD];
+    auto fetch = [&](int e, int p0) {
+        const int r = min(e / QUADS, rows - 1), d = (e % QUADS) * 4;
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            if (p0 - g + u * groups >= it.parts) break;
+            const uint32_t k = at(min(p0 + u * groups, it.parts - 1), r);
+            m[u] = get1(ml, k * 8);
+            x[u] = get2(o, (k * D + d) * 4);
+            y[u] = get2(o, (k * D + d + 2) * 4);
+        }
+    };
+    fetch(e_first, g);
+    {   // maximum and sum of each row: 1 to 64 lanes a row
+        const int lanes = min(64, max(1, THREADS / pow2)), r = min(tid / lanes, rows - 1);
+        float top = -INFINITY, l = 0.f;
+        for (int p = tid % lanes; p < it.parts; p += lanes) {
+            const float2 v = get2(ml, at(p, r) * 8);
+            const float n = fmaxf(top, v.x);
+            l = n > -INFINITY ? l * exp2f(top - n) + v.y * exp2f(v.x - n) : l + v.y;      // the latter 0, or NaN
+            top = n;
+        }
+        for (int d = lanes / 2; d > 0; d >>= 1) {
+            const float m2 = __shfl_xor(top, d), l2 = __shfl_xor(l, d), n = fmaxf(top, m2);
+            l = n > -INFINITY ? l * exp2f(top - n) + l2 * exp2f(m2 - n) : l + l2;
+            top = n;
+        }
+        if (tid % lanes == 0 && tid / lanes < rows) {
+            sh.m[r] = top == -INFINITY ? 0.f : top;
+            sh.l[r] = l;
+            if (a.q.lse) {
+                const int row = it.tile * tile_rows + r, tok = row / a.group;
+                a.q.lse[(int64_t)(it.row0 + tok) * heads * a.group + head * a.group + row - tok * a.group] = l == 0.f ? -INFINITY : LN2 * (top + log2f(l));
+            }
+        }
+    }
+    __syncthreads();
+    for (int e0 = 0; e0 < rows * QUADS; e0 += THREADS) {
+        const int e = e0 + e_first, r = min(e / QUADS, rows - 1), d = (e % QUADS) * 4;
+        const float top = sh.m[r];
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int p0 = g; p0 < it.parts; p0 += AHEAD * groups) {
+            if (e0 || p0 != g) fetch(e, p0);
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                if (p0 - g + u * groups >= it.parts) break;
+                const float w = p0 + u * groups < it.parts ? exp2f(m[u] - top) : 0.f;
+                sum.x = fmaf(w, x[u].x, sum.x);
+                sum.y = fmaf(w, x[u].y, sum.y);
+                sum.z = fmaf(w, y[u].x, sum.z);
+                sum.w = fmaf(w, y[u].y, sum.w);
+            }
+        }
+        if (groups > 1) {
+            sh.sum[tid] = sum;
+            __syncthreads();
+            for (int w = 1; w < groups && g == 0; ++w) {
+                const float4 z = sh.sum[w * all + e];
+                sum.x += z.x;
+                sum.y += z.y;
+                sum.z += z.z;
+                sum.w += z.w;
+            }
+        }
+        if (g == 0 && e < rows * QUADS) {
+            const float l = sh.l[r], f = l == 0.f ? 0.f : 1.f / l;
+            const int row = it.tile * tile_rows + r, tok = row / a.group;
+            store4<DTYPE>(a.q.out, (it.row0 + tok) * a.q.out_stride + (int64_t)(head * a.group + row - tok * a.group) * D + d, a.vec_out, sum.x * f, sum.y * f, sum.z * f, sum.w * f);
+        }
+    }
+}
+
+// ---- a tile of 32 rows: every wave takes every eighth step of the block's, straight from memory into registers
 template <int D>
 struct FewShared {
-    float m[4][ROWS_FEW], l[4][ROWS_FEW];
-    float o[4][ROWS_FEW][33];
+    float m[attend_waves(D)][ROWS_FEW], l[attend_waves(D)][ROWS_FEW];
+    __align__(16) float o[attend_waves(D) * 8 * (D + 4)];
+    JoinShared join;
 };
 
 template <int DTYPE, int FMT, int D>
 __device__ __forceinline__ void attend_few(const AttendArgs &a, const Item &it, int head, FewShared<D> &sh)
 {
+    constexpr int WAVES = attend_waves(D);
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 31, h = lane >> 5;
-    const int rows = it.n_new * a.group;
+    const int rows = it.n_new * a.group, row0 = it.tile * ROWS_FEW, here = min(ROWS_FEW, rows - row0);
+    const Row row = row_at(a, row0, row0 + col, rows);
     v8h q[D / 16];
     float unit;
-    load_queries<DTYPE, D>(a, it, head, col, rows, q, unit);
-    const Sees see = sees(a, it, col, rows);
+    load_queries<DTYPE, D>(a, it, head, row, q, unit);
+    const Sees see = sees(a, it, row);
     const float factor = a.q.scale * LOG2E * unit;
-    // all rows see tokens [all_lo, all_hi); any row sees some of [any_lo, any_hi)
-    const int any_lo = a.window > 0 ? max(0, it.ctx + 1 - a.window) : 0, any_hi = it.ctx + it.n_new;
-    const int all_lo = a.window > 0 ? max(0, it.ctx + it.n_new - a.window) : 0, all_hi = a.causal ? it.ctx + 1 : any_hi;
+    // all rows see tokens [all_lo, all_hi); values below any_lo may lie in pages that the request has given back
+    const int pos_a = it.ctx + __builtin_amdgcn_readlane(row.tok, 0), pos_z = it.ctx + __builtin_amdgcn_readlane(row.tok, here - 1), any_hi = it.ctx + it.n_new;
+    const int any_lo = a.window > 0 ? max(0, pos_a + 1 - a.window) : 0;
+    const int all_lo = a.window > 0 ? max(0, pos_z + 1 - a.window) : 0, all_hi = a.causal ? pos_a + 1 : any_hi;
     State<D> s;
     clear(s);
 
@@ -251,12 +440,12 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, const Item &it, 
     const int kh = (col >> 2) & 1, ktok = 4 * (col >> 3) + (col & 3);     // S^T row `col` is token 16 kh + ktok of the step
     const uint8_t *kbase = static_cast<const uint8_t *>(a.c.k), *vbase = static_cast<const uint8_t *>(a.c.v);
     constexpr int BATCH = 32;       // steps of a wave whose places the lanes hold, two sub-blocks a step
-    for (int first = it.kt0 + wave; first < it.kt1; first += 4 * BATCH) {
-        const int n = min(BATCH, (it.kt1 - first + 3) / 4);
-        const Place mine = (lane >> 1) < n ? place_of(a, it, head, 2 * (first + 4 * (lane >> 1)) + (lane & 1), any_hi) : Place{-1, 1.f, 1.f};
+    for (int first = it.kt0 + wave; first < it.kt1; first += WAVES * BATCH) {
+        const int n = min(BATCH, div_up(it.kt1 - first, WAVES));
+        const Place mine = (lane >> 1) < n ? place_of(a, it, head, 2 * (first + WAVES * (lane >> 1)) + (lane & 1), any_hi) : Place{-1, 1.f, 1.f};
         uint4 k[2][D / 32], v[2][D / 32];
         auto fetch = [&](int j, uint4 (&kk)[D / 32], uint4 (&vv)[D / 32]) {
-            const int kt = first + 4 * j;
+            const int kt = first + WAVES * j;
             const int id0 = max(__builtin_amdgcn_readlane(mine.id, 2 * j), 0), id1 = max(__builtin_amdgcn_readlane(mine.id, 2 * j + 1), 0);
             const int64_t at0 = (((int64_t)id0 * heads + head) * subs + ((2 * kt) & (subs - 1))) * sub_bytes;
             const int64_t at1 = (((int64_t)id1 * heads + head) * subs + ((2 * kt + 1) & (subs - 1))) * sub_bytes;
@@ -268,7 +457,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, const Item &it, 
             for (int i = 0; i < D / 32; ++i) vv[i] = *reinterpret_cast<const uint4 *>(vp + i * 512);
         };
         auto use = [&](int j, uint4 (&kk)[D / 32], uint4 (&vv)[D / 32]) {
-            const int kt = first + 4 * j;
+            const int kt = first + WAVES * j;
             const int src = 2 * j + h;
             const int id = __shfl(mine.id, src);
             const float ks = __shfl(mine.ks, src), vs = __shfl(mine.vs, src);
@@ -283,14 +472,14 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, const Item &it, 
             }
             step<FMT, D>(s, q, kk, vv, factor * ks, __builtin_amdgcn_logf(vs), __builtin_amdgcn_rcpf(vs), edge, tok0, mask);
         };
+        // No branch around a load (past the end the last step is requested again): the compiler then waits for the step it
+        // needs alone, with the next one's loads in flight.
         fetch(0, k[0], v[0]);
         for (int j = 0; j < n; j += 2) {
-            if (j + 1 < n) fetch(j + 1, k[1], v[1]);
+            fetch(min(j + 1, n - 1), k[1], v[1]);
             use(j, k[0], v[0]);
-            if (j + 1 < n) {
-                if (j + 2 < n) fetch(j + 2, k[0], v[0]);
-                use(j + 1, k[1], v[1]);
-            }
+            fetch(min(j + 2, n - 1), k[0], v[0]);
+            if (j + 1 < n) use(j + 1, k[1], v[1]);
         }
     }
     // join the waves
@@ -300,87 +489,106 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, const Item &it, 
         sh.l[wave][col] = s.l;
     }
     __syncthreads();
-    const float top = fmaxf(fmaxf(sh.m[0][col], sh.m[1][col]), fmaxf(sh.m[2][col], sh.m[3][col]));
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, sh.m[w][col]);
     const float base = top == -INFINITY ? 0.f : top;
     float l = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) l += sh.l[w][col] * exp2f(sh.m[w][col] - base);
+    for (int w = 0; w < WAVES; ++w) l += sh.l[w][col] * exp2f(sh.m[w][col] - base);
     float f = exp2f(s.m - base);
     const bool whole = it.part < 0;
     if (whole) f = l == 0.f ? 0.f : f / l;
     const int64_t part = ((int64_t)it.part * heads + head) * ROWS_FEW;
-    if (tid < ROWS_FEW && tid < rows) {
-        if (!whole) {
-            float *ml = a.part_few + (int64_t)a.p.parts_few * heads * ROWS_FEW * D + (part + tid) * 2;
-            ml[0] = top;
-            ml[1] = l;
-        } else if (a.q.lse) {
-            a.q.lse[(int64_t)(it.row0 + tid / a.group) * heads * a.group + head * a.group + tid % a.group] = LN2 * (top + log2f(l));
-        }
+    float *ml = a.part_few + (int64_t)a.p.parts_few * heads * ROWS_FEW * D;
+    if (tid < here) {
+        if (!whole) put2(ml + (part + tid) * 2, top, l);
+        else if (a.q.lse) a.q.lse[(int64_t)(it.row0 + row.tok) * heads * a.group + head * a.group + row.g] = LN2 * (top + log2f(l));
     }
+    // as many rows at a time as the waves' outputs of them fit into LDS: all of a token's where its group has eight heads or fewer
+    constexpr int STRIDE = D + 4, HOLD = sizeof(sh.o) / (WAVES * STRIDE * 4), QUADS = D / 4;
+    for (int r0 = 0; r0 < here; r0 += HOLD) {
+        if (r0) __syncthreads();
+        if (col >= r0 && col < min(r0 + HOLD, here)) {
 #pragma unroll
-    for (int n = 0; n < D / 32; ++n) {
-        if (n) __syncthreads();
+            for (int n = 0; n < D / 32; ++n)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sh.o[wave][col][8 * (i / 4) + 4 * h + i % 4] = s.o[n][i] * f;
+                for (int i = 0; i < 4; ++i)
+                    *reinterpret_cast<float4 *>(sh.o + (wave * HOLD + col - r0) * STRIDE + 32 * n + 8 * i + 4 * h) =
+                        make_float4(s.o[n][4 * i] * f, s.o[n][4 * i + 1] * f, s.o[n][4 * i + 2] * f, s.o[n][4 * i + 3] * f);
+        }
         __syncthreads();
-        const int r = tid >> 3, d = (tid & 7) * 4;
-        if (r < rows) {
-            float x[4];
+        for (int e = tid; e < min(HOLD, here - r0) * QUADS; e += 64 * WAVES) {
+            const int r = e / QUADS, d = (e % QUADS) * 4;
+            float4 x = *reinterpret_cast<const float4 *>(sh.o + r * STRIDE + d);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = (sh.o[0][r][d + i] + sh.o[1][r][d + i]) + (sh.o[2][r][d + i] + sh.o[3][r][d + i]);
+            for (int w = 1; w < WAVES; ++w) {
+                const float4 y = *reinterpret_cast<const float4 *>(sh.o + (w * HOLD + r) * STRIDE + d);
+                x.x += y.x;
+                x.y += y.y;
+                x.z += y.z;
+                x.w += y.w;
+            }
             if (whole) {
-                const int tok = r / a.group, g = r - tok * a.group;
-                store4<DTYPE>(a.q.out, (it.row0 + tok) * a.q.out_stride + (int64_t)(head * a.group + g) * D + n * 32 + d, a.vec_out, x[0], x[1], x[2], x[3]);
+                const Row out = row_at(a, row0, row0 + r0 + r, rows);
+                store4<DTYPE>(a.q.out, (it.row0 + out.tok) * a.q.out_stride + (int64_t)(head * a.group + out.g) * D + d, a.vec_out, x.x, x.y, x.z, x.w);
             } else {
-                *reinterpret_cast<float4 *>(a.part_few + (part + r) * D + n * 32 + d) = make_float4(x[0], x[1], x[2], x[3]);
+                float *p = a.part_few + (part + r0 + r) * D + d;
+                put2(p, x.x, x.y);
+                put2(p + 2, x.z, x.w);
             }
         }
     }
+    if (!whole && all_parts_done(a.p.joins_few + it.join * heads + head, it.parts, sh.join)) join_parts<DTYPE, D>(a, it, head, a.part_few, ml, ROWS_FEW, sh.join);
 }
 
-// ---- tiles of 128 rows: every wave has 32 of them, all waves share the block's steps through LDS, two steps at a time
+// ---- tiles of 32 rows a wave: every wave has its own, all waves share the block's steps through LDS, two steps at a time
 template <int D>
 struct ManyShared {
     static constexpr int PLACES = 256;      // sub-blocks whose places are known at a time
     uint4 k[2][4 * D], v[2][4 * D];         // [buffer][sub-block of the two steps][pieces]
     Place place[PLACES];
+    JoinShared join;
 };
 
 template <int DTYPE, int FMT, int D>
 __device__ __forceinline__ void attend_many(const AttendArgs &a, const Item &it, int head, ManyShared<D> &sh)
 {
+    constexpr int THREADS = 64 * attend_waves(D), ROWS = 32 * attend_waves(D);
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 31, h = lane >> 5;
-    const int rows = it.n_new * a.group, row0 = it.tile * ROWS_MANY + wave * 32, row = row0 + col;
+    const int rows = it.n_new * a.group, tile0 = it.tile * ROWS, row0 = tile0 + wave * 32;
+    const Row row = row_at(a, tile0, row0 + col, rows);
     v8h q[D / 16];
     float unit;
-    load_queries<DTYPE, D>(a, it, head, row, rows, q, unit);
-    const Sees see = sees(a, it, row, rows);
+    load_queries<DTYPE, D>(a, it, head, row, q, unit);
+    const Sees see = sees(a, it, row);
     const float factor = a.q.scale * LOG2E * unit;
-    const int pos_a = it.ctx + min(row0, rows - 1) / a.group, pos_z = it.ctx + min(row0 + 31, rows - 1) / a.group;
+    const int pos_a = it.ctx + __builtin_amdgcn_readlane(row.tok, 0), pos_z = it.ctx + __builtin_amdgcn_readlane(row.tok, max(0, min(31, rows - 1 - row0)));
     const int end = it.ctx + it.n_new;
     const int any_lo = a.window > 0 ? max(0, pos_a + 1 - a.window) : 0, any_hi = row0 >= rows ? 0 : a.causal ? pos_z + 1 : end;
     const int all_lo = a.window > 0 ? max(0, pos_z + 1 - a.window) : 0, all_hi = a.causal ? pos_a + 1 : end;
     // values before this one may lie in pages that the request has given back
-    const int tile_lo = a.window > 0 ? max(0, it.ctx + it.tile * ROWS_MANY / a.group + 1 - a.window) : 0;
+    const int tile_lo = a.window > 0 ? max(0, it.ctx + it.tile * ROWS / a.group + 1 - a.window) : 0;
     State<D> s;
     clear(s);
 
     const int heads = a.c.kv_heads, subs = a.c.page / SUB;
     const int kh = (col >> 2) & 1, ktok = 4 * (col >> 3) + (col & 3);
     const uint4 *kbase = static_cast<const uint4 *>(a.c.k), *vbase = static_cast<const uint4 *>(a.c.v);
-    constexpr int PER = 4 * D / ATTEND_THREADS;     // pieces of 16 bytes of a thread: two steps hold 4 D of each kind
+    constexpr int PER = div_up(4 * D, THREADS);     // pieces of 16 bytes of a thread: two steps hold 4 D of each kind
+    const bool loads = 4 * D >= THREADS || tid < 4 * D;
     for (int batch = it.kt0; batch < it.kt1; batch += ManyShared<D>::PLACES / 2) {
         const int last = min(it.kt1, batch + ManyShared<D>::PLACES / 2);
         __syncthreads();
-        for (int i = tid; i < 2 * (last - batch) + 2; i += ATTEND_THREADS)
+        for (int i = tid; i < 2 * (last - batch) + 2; i += THREADS)
             if (i < ManyShared<D>::PLACES) sh.place[i] = place_of(a, it, head, 2 * batch + i, end);
         __syncthreads();
         uint4 rk[PER], rv[PER];
         auto fetch = [&](int kt) {
+            if (!loads) return;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int piece = tid + i * ATTEND_THREADS, sb = piece / D, in = piece - sb * D;
+                const int piece = tid + i * THREADS, sb = piece / D, in = piece - sb * D;
                 const int idx = 2 * (kt - batch) + sb;
                 const int id = idx < ManyShared<D>::PLACES && kt + sb / 2 < last ? max(sh.place[idx].id, 0) : 0;
                 const int64_t at = (((int64_t)id * heads + head) * subs + ((2 * kt + sb) & (subs - 1))) * D + in;
@@ -389,10 +597,11 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const Item &it,
             }
         };
         auto put = [&](int buf) {
+            if (!loads) return;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                sh.k[buf][tid + i * ATTEND_THREADS] = rk[i];
-                sh.v[buf][tid + i * ATTEND_THREADS] = rv[i];
+                sh.k[buf][tid + i * THREADS] = rk[i];
+                sh.v[buf][tid + i * THREADS] = rv[i];
             }
         };
         fetch(batch);
@@ -430,119 +639,55 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const Item &it,
         }
     }
     s.l += __shfl_xor(s.l, 32);
-    if (row >= rows) return;
     const bool whole = it.part < 0;
-    const int tok = row / a.group, g = row - tok * a.group;
-    const int64_t part = ((int64_t)it.part * heads + head) * ROWS_MANY + wave * 32 + col;
-    const float f = whole ? (s.l == 0.f ? 0.f : 1.f / s.l) : 1.f;
-    const int64_t out = (it.row0 + tok) * a.q.out_stride + (int64_t)(head * a.group + g) * D;
+    float *ml = a.part_many + (int64_t)a.p.parts_many * heads * ROWS * D;
+    if (row.real) {
+        const int tok = row.tok, g = row.g;
+        const int64_t part = ((int64_t)it.part * heads + head) * ROWS + wave * 32 + col;
+        const float f = whole ? (s.l == 0.f ? 0.f : 1.f / s.l) : 1.f;
+        const int64_t out = (it.row0 + tok) * a.q.out_stride + (int64_t)(head * a.group + g) * D;
 #pragma unroll
-    for (int n = 0; n < D / 32; ++n)
+        for (int n = 0; n < D / 32; ++n)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int d = 32 * n + 8 * i + 4 * h;
-            const float x = s.o[n][4 * i] * f, y = s.o[n][4 * i + 1] * f, z = s.o[n][4 * i + 2] * f, w = s.o[n][4 * i + 3] * f;
-            if (whole) store4<DTYPE>(a.q.out, out + d, a.vec_out, x, y, z, w);
-            else *reinterpret_cast<float4 *>(a.part_many + part * D + d) = make_float4(x, y, z, w);
-        }
-    if (h == 0) {
-        if (!whole) {
-            float *ml = a.part_many + (int64_t)a.p.parts_many * heads * ROWS_MANY * D + part * 2;
-            ml[0] = s.m;
-            ml[1] = s.l;
-        } else if (a.q.lse) {
-            a.q.lse[(int64_t)(it.row0 + tok) * heads * a.group + head * a.group + g] = s.l == 0.f ? -INFINITY : LN2 * (s.m + log2f(s.l));
+            for (int i = 0; i < 4; ++i) {
+                const int d = 32 * n + 8 * i + 4 * h;
+                const float x = s.o[n][4 * i] * f, y = s.o[n][4 * i + 1] * f, z = s.o[n][4 * i + 2] * f, w = s.o[n][4 * i + 3] * f;
+                if (whole) {
+                    store4<DTYPE>(a.q.out, out + d, a.vec_out, x, y, z, w);
+                } else {
+                    put2(a.part_many + part * D + d, x, y);
+                    put2(a.part_many + part * D + d + 2, z, w);
+                }
+            }
+        if (h == 0) {
+            if (!whole) put2(ml + part * 2, s.m, s.l);
+            else if (a.q.lse) a.q.lse[(int64_t)(it.row0 + tok) * heads * a.group + head * a.group + g] = s.l == 0.f ? -INFINITY : LN2 * (s.m + log2f(s.l));
         }
     }
+    if (!whole && all_parts_done(a.p.joins_many + it.join * heads + head, it.parts, sh.join)) join_parts<DTYPE, D>(a, it, head, a.part_many, ml, ROWS, sh.join);
 }
 
 template <int DTYPE, int FMT, int D>
-__global__ void __launch_bounds__(ATTEND_THREADS, D <= 128 ? 2 : 1) k_kv_attend(AttendArgs a)
+__global__ void __launch_bounds__(64 * attend_waves(D), D <= 128 ? 2 : 1) k_kv_attend(AttendArgs a)
 {
     __shared__ union {
         FewShared<D> few;
         ManyShared<D> many;
     } sh;
+    // kv heads follow each other: blocks of one head, which share cached tokens, come to the same die where there are eight
     const int heads = a.c.kv_heads;
     if ((int)blockIdx.x < a.many_blocks) {
         const int i = blockIdx.x / heads;
-        if (i >= a.p.head->many) return;
-        attend_many<DTYPE, FMT, D>(a, a.p.many[i], blockIdx.x % heads, sh.many);
+        const Item it = item_at(a.p.many + i);      // in flight with the list's length; past it it is whatever was there
+        if (i < a.p.head->many) attend_many<DTYPE, FMT, D>(a, it, blockIdx.x - i * heads, sh.many);
     } else {
         const int b = blockIdx.x - a.many_blocks, i = b / heads;
-        if (i >= a.p.head->few) return;
-        attend_few<DTYPE, FMT, D>(a, a.p.few[i], b % heads, sh.few);
-    }
-}
-
-// Joins the partial results of rows that were split: JOIN_ROWS rows of one tile and head a block.
-constexpr int JOIN_THREADS = 512, JOIN_ROWS = 4;
-
-template <int DTYPE>
-__global__ void __launch_bounds__(JOIN_THREADS) k_kv_join(AttendArgs a, int many, int tile_rows, int chunks)
-{
-    __shared__ float red_m[JOIN_ROWS][2], red_l[JOIN_ROWS][2];
-    __shared__ float4 red_o[JOIN_THREADS];
-    const int tid = threadIdx.x, heads = a.c.kv_heads, D = a.c.head_dim;
-    const int chunk = blockIdx.x % chunks, head = (blockIdx.x / chunks) % heads, i = blockIdx.x / chunks / heads;
-    if (i >= (many ? a.p.head->joins_many : a.p.head->joins_few)) return;
-    const Join j = (many ? a.p.joins_many : a.p.joins_few)[i];
-    const int rows = min(tile_rows, j.n_new * a.group - j.tile * tile_rows), r0 = chunk * JOIN_ROWS;
-    if (r0 >= rows) return;
-    const float *o = many ? a.part_many : a.part_few;
-    const float2 *ml = reinterpret_cast<const float2 *>(o + (int64_t)(many ? a.p.parts_many : a.p.parts_few) * heads * tile_rows * D);
-    auto at = [&](int p, int r) { return ((int64_t)(j.part0 + p) * heads + head) * tile_rows + r; };
-    // maximum and sum of each row: 128 threads a row
-    {
-        const int rr = tid >> 7, r = min(r0 + rr, rows - 1);
-        float m = -INFINITY, l = 0.f;
-        for (int p = tid & 127; p < j.parts; p += 128) {
-            const float2 x = ml[at(p, r)];
-            const float n = fmaxf(m, x.x);
-            if (n > -INFINITY) l = l * exp2f(m - n) + x.y * exp2f(x.x - n);
-            else l += x.y;              // 0, or NaN
-            m = n;
+        const int first = a.p.few_first[i], last = a.p.few_first[i + 1];
+        if (i >= a.p.head->few_blocks) return;
+        for (int k = first; k < last; ++k) {
+            if (k > first) __syncthreads();          // the item before is done with LDS
+            attend_few<DTYPE, FMT, D>(a, item_at(a.p.few + k), b - i * heads, sh.few);
         }
-        for (int d = 32; d > 0; d >>= 1) {
-            const float m2 = __shfl_xor(m, d), l2 = __shfl_xor(l, d), n = fmaxf(m, m2);
-            l = n > -INFINITY ? l * exp2f(m - n) + l2 * exp2f(m2 - n) : l + l2;
-            m = n;
-        }
-        if ((tid & 63) == 0) {
-            red_m[rr][(tid >> 6) & 1] = m;
-            red_l[rr][(tid >> 6) & 1] = l;
-        }
-    }
-    __syncthreads();
-    const int quads = D / 4, per = JOIN_ROWS * quads, groups = JOIN_THREADS / per;     // D = 64, 128, 256: 8, 4, 2 groups
-    const int e = tid % per, g = tid / per, rr = e / quads, d = (e % quads) * 4, r = min(r0 + rr, rows - 1);
-    const float top = fmaxf(red_m[rr][0], red_m[rr][1]), base = top == -INFINITY ? 0.f : top;
-    const float l = red_l[rr][0] * exp2f(red_m[rr][0] - base) + red_l[rr][1] * exp2f(red_m[rr][1] - base);
-    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int p = g; p < j.parts; p += groups) {
-        const int64_t k = at(p, r);
-        const float w = exp2f(ml[k].x - base);
-        const float4 x = *reinterpret_cast<const float4 *>(o + k * D + d);
-        sum.x += w * x.x;
-        sum.y += w * x.y;
-        sum.z += w * x.z;
-        sum.w += w * x.w;
-    }
-    red_o[tid] = sum;
-    __syncthreads();
-    if (tid < per && r0 + rr < rows) {
-        for (int w = 1; w < groups; ++w) {
-            const float4 x = red_o[w * per + tid];
-            sum.x += x.x;
-            sum.y += x.y;
-            sum.z += x.z;
-            sum.w += x.w;
-        }
-        const float f = l == 0.f ? 0.f : 1.f / l;
-        const int row = j.tile * tile_rows + r0 + rr, tok = row / a.group, q = head * a.group + row % a.group;
-        store4<DTYPE>(a.q.out, (j.row0 + tok) * a.q.out_stride + (int64_t)q * D + d, a.vec_out, sum.x * f, sum.y * f, sum.z * f, sum.w * f);
-        if (a.q.lse && d == 0) a.q.lse[(int64_t)(j.row0 + tok) * heads * a.group + q] = l == 0.f ? -INFINITY : LN2 * (top + log2f(l));
     }
 }
 

@@ -14,21 +14,22 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 
 constexpr int SUB = 16;            // tokens of a 16 x 16 tile of codes
 constexpr int KT = 32;             // tokens of a step of the attention kernels: the rows of one matrix instruction
+// Waves of a block of the attention: two on every SIMD of a compute unit; heads of 256 take the registers of both for one.
+__host__ __device__ constexpr int attend_waves(int head_dim) { return head_dim <= 128 ? 4 : 4; }
 constexpr int ROWS_FEW = 32;       // (token, query head of the group) rows of a block whose waves share out the cached tokens
-constexpr int ROWS_MANY = 128;     // ... and of one whose waves share out the rows
-constexpr int BLOCKS_FEW = 1024;   // blocks that the cached tokens of small requests are shared out to at most, beyond one a request
+constexpr int FEW_MOST = 64;       // requests of up to this many rows are made of such blocks; the others of blocks whose waves
+                                   // share out the rows, 32 to each
+constexpr int COMPUTE_UNITS = 256;
+constexpr int BLOCKS_FEW = 2 * COMPUTE_UNITS;    // blocks that the cached tokens of small requests are shared out to: two a compute unit
 constexpr int BLOCKS_MANY = 512;
-constexpr int MIN_KT_FEW = 8;      // steps of a block at least where a request is split
+constexpr int MIN_KT_FEW = 32;     // steps of a block at least
 constexpr int MIN_KT_MANY = 16;
 
-// One block's work, for each kv head: rows [tile * ROWS, ...) of a request against the cached tokens [kt0, kt1) * KT.
+// A piece of work, for each kv head: rows [tile * ROWS, ...) of a request against the cached tokens [kt0, kt1) * KT.
 struct __align__(16) Item {
     int32_t req, row0, n_new, ctx;      // row0: first packed row of the request; ctx: position of its token
     int32_t tile, kt0, kt1, part;       // part: which partial result, -1: the block holds all and writes the output
-};
-struct __align__(16) Join {
-    int32_t row0, n_new, tile, part0;
-    int32_t parts, pad[3];
+    int32_t part0, parts, join, pad;    // the parts that belong together, and where those that are done are counted
 };
 // New tokens of one page.
 struct __align__(16) Segment {
@@ -36,7 +37,7 @@ struct __align__(16) Segment {
     int32_t pos0, pad[3];
 };
 struct Header {
-    int32_t segments, few, many, joins_few, joins_many, pad[11];
+    int32_t segments, few_blocks, many, pad[13];
 };
 
 // Where a plan's lists lie in its buffer, and how long they can get.
@@ -45,11 +46,12 @@ struct Plan {
     int32_t *positions;
     Segment *segments;
     Item *few, *many;
-    Join *joins_few, *joins_many;
-    int32_t max_segments, max_few, max_many, max_joins_few, max_joins_many, parts_few, parts_many;
+    int32_t *few_first;                 // [few_blocks + 1]: the items of a block of small requests are [few_first[b], few_first[b + 1])
+    int32_t *joins_few, *joins_many;    // [join][kv head]: parts that are done; 0 between launches
+    int32_t max_segments, blocks_few, max_few, max_many, max_joins_few, max_joins_many, parts_few, parts_many;
 };
 
-__host__ __device__ inline int div_up(int a, int b) { return (a + b - 1) / b; }
+__host__ __device__ constexpr int div_up(int a, int b) { return (a + b - 1) / b; }
 
 // a new float from its sixteen bits
 template <int DTYPE>

@@ -19,7 +19,7 @@ struct PlanArgs {
     moe_kv_step_t s;
     moe_kv_lists_t io;
     Plan p;
-    int32_t group, page_shift, target_few, target_many;
+    int32_t group, page_shift, target_few, target_many, rows_many;
 };
 
 // a + b, 2^32 - 1 at most: sums of lengths that no batch can have stay above every bound they are compared with
@@ -103,11 +103,13 @@ __device__ __forceinline__ int share(double all, int target, int least)
     return max(least, (int)(((int64_t)all + target - 1) / target));
 }
 
-// Writes the items of one unit of work, in as many parts as `n`, and what joins them.
-__device__ __forceinline__ void put_items(Item *items, Join *joins, Item it, int n, int item0, int join0, int part0)
+// Writes the items of one tile, in as many parts as `n`.
+__device__ __forceinline__ void put_items(Item *items, Item it, int n, int item0, int join, int part0)
 {
     const int lo = it.kt0, len = it.kt1 - it.kt0;
-    if (n > 1) joins[join0] = Join{it.row0, it.n_new, it.tile, part0, n, {0, 0, 0}};
+    it.part0 = part0;
+    it.parts = n;
+    it.join = join;
     for (int p = 0; p < n; ++p) {
         it.kt0 = lo + (int)((int64_t)len * p / n);
         it.kt1 = lo + (int)((int64_t)len * (p + 1) / n);
@@ -184,60 +186,92 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
     if (role == 0) {
         // what is per request, and the requests of few rows
         block_scan<THREADS>(used, tmp, &total);
-        Item it[PER];
-        double steps = 0.0;
+        // Tiles of 32 rows, one after the other on a line of steps (a tile that sees nothing takes one step of it): every
+        // block gets a piece of the line of the same length, whatever tiles begin and end in it.  A tile that lies in several
+        // pieces is joined from its parts.  Sums stay below 2^32: 8192 tiles of less than 2^19 steps.
+        auto tiles_of = [&](int i) {
+            const int rows = now[i] * a.group;
+            return rows > FEW_MOST || st[i] == MOE_KV_BAD_SIZE ? 0 : div_up(rows, ROWS_FEW);
+        };
+        auto item_of = [&](int i, int tile) {
+            Item it{r0 + i, first[i], now[i], ctx[i], tile, 0, 0, -1, 0, 0, 0, 0};
+            if (!st[i]) key_steps(s, ctx[i], now[i], tile * ROWS_FEW / a.group, (min((tile + 1) * ROWS_FEW, now[i] * a.group) - 1) / a.group, it.kt0, it.kt1);
+            return it;
+        };
+        uint32_t steps = 0, line;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int r = r0 + i, rows = now[i] * a.group;
-            it[i] = Item{r, first[i], rows == 0 || rows > ROWS_FEW || st[i] == MOE_KV_BAD_SIZE ? 0 : now[i], ctx[i], 0, 0, 0, -1};
+            const int r = r0 + i;
             if (i < per && r < R) {
                 a.io.row_start[r + 1] = first[i] + now[i];
                 a.io.kv_len[r] = st[i] ? ctx[i] : ctx[i] + now[i];
                 a.io.status[r] = st[i];
-                if (it[i].n_new && !st[i]) key_steps(s, ctx[i], now[i], 0, now[i] - 1, it[i].kt0, it[i].kt1);
             }
-            steps += it[i].kt1 - it[i].kt0;
+            for (int t = 0; t < tiles_of(i); ++t) {
+                const Item it = item_of(i, t);
+                steps += max(1, it.kt1 - it.kt0);
+            }
         }
         if (tid == 0) {
             a.io.row_start[0] = 0;
             a.io.free_left[0] = free_n - (int)total;
         }
-        const int chunk = share(block_sum<THREADS>(steps, tmp_d), a.target_few, MIN_KT_FEW);
-        uint32_t items = 0, split = 0;                   // split: joins << 16 | parts
-        int n[PER];
+        const uint32_t start = block_scan<THREADS>(steps, tmp, &line) - steps;
+        const uint32_t chunk = max((uint32_t)MIN_KT_FEW, (line + a.target_few - 1) / a.target_few);
+        uint32_t items = 0, split = 0, pos = start;      // split: joins << 16 | parts
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            n[i] = it[i].n_new ? max(1, div_up(it[i].kt1 - it[i].kt0, chunk)) : 0;
-            items += n[i];
-            split += n[i] > 1 ? (1u << 16) + n[i] : 0;
-        }
+        for (int i = 0; i < PER; ++i)
+            for (int t = 0; t < tiles_of(i); ++t) {
+                const Item it = item_of(i, t);
+                const uint32_t len = max(1, it.kt1 - it.kt0), n = (pos + len - 1) / chunk - pos / chunk + 1;
+                items += n;
+                split += n > 1 ? (1u << 16) + n : 0;
+                pos += len;
+            }
         uint32_t all_items, all_split;
         uint32_t item0 = block_scan<THREADS>(items, tmp, &all_items) - items, split0 = block_scan<THREADS>(split, tmp, &all_split) - split;
+        pos = start;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            put_items(a.p.few, a.p.joins_few, it[i], n[i], item0, split0 >> 16, split0 & 0xFFFF);
-            item0 += n[i];
-            split0 += n[i] > 1 ? (1u << 16) + n[i] : 0;
-        }
+        for (int i = 0; i < PER; ++i)
+            for (int t = 0; t < tiles_of(i); ++t) {
+                Item it = item_of(i, t);
+                const int len = it.kt1 - it.kt0, kt0 = it.kt0;
+                const uint32_t b0 = pos / chunk, n = (pos + max(1, len) - 1) / chunk - b0 + 1;
+                it.part0 = split0 & 0xFFFF;
+                it.parts = n;
+                it.join = split0 >> 16;
+                for (uint32_t p = 0; p < n; ++p) {
+                    const int at = (int)((b0 + p) * chunk - pos);        // where the block's piece begins, from the tile's first step
+                    it.kt0 = kt0 + max(0, at);
+                    it.kt1 = kt0 + min(len, at + (int)chunk);
+                    it.part = n > 1 ? it.part0 + p : -1;
+                    a.p.few[item0 + p] = it;
+                    if (at >= 0) a.p.few_first[b0 + p] = item0 + p;      // the block's first item
+                }
+                item0 += n;
+                split0 += n > 1 ? (1u << 16) + n : 0;
+                pos += max(1, len);
+            }
         if (tid == 0) {
-            a.p.head->few = (int)all_items;
-            a.p.head->joins_few = (int)(all_split >> 16);
+            const uint32_t blocks = (line + chunk - 1) / chunk;
+            a.p.head->few_blocks = (int)blocks;
+            a.p.few_first[blocks] = (int)all_items;
         }
         return;
     }
     if (role == 1) {
-        // Tiles of 128 rows of the other requests.  A request of a bad size has none: it may have more rows than the lists
+        // Tiles of the other requests.  A request of a bad size has none: it may have more rows than the lists
         // are made for.
         auto tiles_of = [&](int i) {
             const int rows = now[i] * a.group;
-            return rows <= ROWS_FEW || st[i] == MOE_KV_BAD_SIZE ? 0 : div_up(rows, ROWS_MANY);
+            return rows <= FEW_MOST || st[i] == MOE_KV_BAD_SIZE ? 0 : div_up(rows, a.rows_many);
         };
         uint32_t units = 0, n_units;
 #pragma unroll
         for (int i = 0; i < PER; ++i) units += tiles_of(i);
         uint32_t unit_at = block_scan<THREADS>(units, tmp, &n_units) - units;
         if (n_units == 0) {
-            if (tid == 0) a.p.head->many = a.p.head->joins_many = 0;
+            if (tid == 0) a.p.head->many = 0;
             return;
         }
 #pragma unroll
@@ -256,7 +290,7 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
             it.tile = sums[r] - 1 - u;                   // the last rows see most: they go first
             it.kt0 = it.kt1 = 0;                         // turned down: nothing to attend to
             if (need_before[r] >= 0)
-                key_steps(s, it.ctx, n, it.tile * ROWS_MANY / a.group, (min((it.tile + 1) * ROWS_MANY, n * a.group) - 1) / a.group, it.kt0, it.kt1);
+                key_steps(s, it.ctx, n, it.tile * a.rows_many / a.group, (min((it.tile + 1) * a.rows_many, n * a.group) - 1) / a.group, it.kt0, it.kt1);
         };
         double steps = 0.0;
         for (int u = tid; u < (int)n_units; u += THREADS) {
@@ -278,12 +312,9 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
             const uint32_t item0 = items + block_scan<THREADS>(n, tmp, &all_items) - n, split0 = split + block_scan<THREADS>(mine, tmp, &all_split) - mine;
             items += all_items;
             split += all_split;
-            put_items(a.p.many, a.p.joins_many, it, n, item0, split0 >> 16, split0 & 0xFFFF);
+            put_items(a.p.many, it, n, item0, split0 >> 16, split0 & 0xFFFF);
         }
-        if (tid == 0) {
-            a.p.head->many = (int)items;
-            a.p.head->joins_many = (int)(split >> 16);
-        }
+        if (tid == 0) a.p.head->many = (int)items;
         return;
     }
 
@@ -309,6 +340,7 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
         return a.io.free_pages[free_n - 1 - (need_before[r] + blk - held)];
     };
     const int worker = role - 2, workers = gridDim.x - 2;
+    for (int i = worker * THREADS + tid; i < (a.p.max_joins_few + a.p.max_joins_many) * s.kv_heads; i += workers * THREADS) a.p.joins_few[i] = 0;
     for (int t = worker * THREADS + tid; t < T; t += workers * THREADS) {
         const int r = first_above(row_end, R, t);
         int pos = -1, slot = -1;

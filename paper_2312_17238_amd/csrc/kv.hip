@@ -10,6 +10,7 @@
 #include "../../include/moe_kv.h"
 #include "errors.h"
 #include "kernels_kv_attend.h"
+#include "kernels_kv_decode.h"
 #include "kernels_kv_plan.h"
 #include "kernels_kv_write.h"
 
@@ -38,14 +39,14 @@ static int32_t launched(const char *what)
 static bool geometry_ok(int32_t n_pages, int32_t page, int32_t kv_heads, int32_t head_dim)
 {
     return n_pages >= 1 && (page == 16 || page == 32 || page == 64 || page == 128) && (int64_t)n_pages * page < (1ll << 31) &&
-           kv_heads >= 1 && kv_heads <= 256 && (head_dim == 64 || head_dim == 128 || head_dim == 256);
+           kv_heads >= 1 && kv_heads <= 256 && (int64_t)n_pages * kv_heads * (page / 16) < (1ll << 32) && (head_dim == 64 || head_dim == 128 || head_dim == 256);
 }
 
 static bool step_ok(const moe_kv_step_t *s)
 {
     return s && s->n_requests >= 1 && s->n_requests <= MOE_KV_MAX_REQUESTS && s->n_tokens >= 1 && s->n_tokens <= MOE_KV_MAX_TOKENS &&
            s->max_new >= 1 && s->max_blocks >= 1 && geometry_ok(s->n_pages, s->page, s->kv_heads, s->head_dim) &&
-           (int64_t)s->max_blocks * s->page < (1ll << 30) && s->q_heads >= 1 && s->q_heads <= 1024 && s->q_heads % s->kv_heads == 0 &&
+           (int64_t)s->max_blocks * s->page < (1ll << 24) && s->q_heads >= 1 && s->q_heads <= 1024 && s->q_heads % s->kv_heads == 0 &&
            (s->causal == 0 || s->causal == 1) && s->window >= 0 && s->reserved == 0;
 }
 
@@ -69,9 +70,11 @@ static int log2_of(int v)
 }
 
 struct Sizes {
+    int rows_many;
     int group, new_most;        // new_most: rows that one request can bring
+    bool decode;                // none can have more than ROWS_DECODE
     bool many;                  // some request can have more than ROWS_FEW rows
-    uint64_t segments, positions, few, many_at, joins_few, joins_many, total;
+    uint64_t segments, positions, few, few_first, many_at, joins, total;
     Plan p;                     // counts only
 };
 
@@ -80,21 +83,28 @@ static int target_blocks(int blocks, int heads) { return std::max(1, blocks / he
 static Sizes sizes_of(const moe_kv_step_t *s)
 {
     Sizes z{};
+    z.rows_many = 32 * attend_waves(s->head_dim);
     z.group = s->q_heads / s->kv_heads;
     z.new_most = std::min(s->max_new, s->n_tokens);
-    z.many = (int64_t)z.new_most * z.group > ROWS_FEW;
+    z.many = (int64_t)z.new_most * z.group > FEW_MOST;
+    z.decode = (int64_t)z.new_most * z.group <= ROWS_DECODE;
     const int R = s->n_requests, T = s->n_tokens;
     const int steps = div_up(s->max_blocks * s->page, KT);          // of one request at most
     Plan &p = z.p;
     p.max_segments = (int)std::min<int64_t>(T, (int64_t)T / s->page + 2ll * R);
-    const bool split_few = steps > MIN_KT_FEW, split_many = z.many && steps > MIN_KT_MANY;
-    const int tf = target_blocks(BLOCKS_FEW, s->kv_heads), tm = target_blocks(BLOCKS_MANY, s->kv_heads);
-    p.max_few = std::min(R, T) + (split_few ? tf : 0);
-    const int tiles = z.many ? (int)((int64_t)T * z.group / ROWS_MANY) + std::min(R, T) : 0;
+    const bool split_many = z.many && steps > MIN_KT_MANY;
+    const int tf = target_blocks(z.decode ? COMPUTE_UNITS * decode_blocks(s->head_dim) : BLOCKS_FEW, s->kv_heads), tm = target_blocks(BLOCKS_MANY, s->kv_heads);
+    // tiles: of no request more than its rows, or the most rows of one, fill
+    const int tiles_few = (int)std::min<int64_t>((int64_t)std::min(R, T) * div_up((int)std::min<int64_t>(FEW_MOST, (int64_t)z.new_most * z.group), ROWS_FEW),
+                                                 (int64_t)T * z.group / ROWS_FEW + std::min(R, T));
+    const bool split_few = (int64_t)tiles_few * steps > MIN_KT_FEW;     // more than one block
+    p.blocks_few = split_few ? tf : 1;
+    p.max_few = tiles_few + p.blocks_few;
+    const int tiles = z.many ? (int)((int64_t)T * z.group / z.rows_many) + std::min(R, T) : 0;
     p.max_many = tiles + (split_many ? tm : 0);
     p.parts_few = split_few ? 2 * tf : 0;
     p.parts_many = split_many ? 2 * tm : 0;
-    p.max_joins_few = std::min(std::min(R, T), p.parts_few / 2);
+    p.max_joins_few = std::min(tiles_few, p.parts_few / 2);
     p.max_joins_many = std::min(tiles, p.parts_many / 2);
     uint64_t at = sizeof(Header);
     auto take = [&](uint64_t bytes) {
@@ -105,14 +115,14 @@ static Sizes sizes_of(const moe_kv_step_t *s)
     z.positions = take((uint64_t)T * 4);
     z.segments = take((uint64_t)p.max_segments * sizeof(Segment));
     z.few = take((uint64_t)p.max_few * sizeof(Item));
+    z.few_first = take((uint64_t)(p.blocks_few + 1) * 4);
     z.many_at = take((uint64_t)p.max_many * sizeof(Item));
-    z.joins_few = take((uint64_t)p.max_joins_few * sizeof(Join));
-    z.joins_many = take((uint64_t)p.max_joins_many * sizeof(Join));
+    z.joins = take((uint64_t)(p.max_joins_few + p.max_joins_many) * s->kv_heads * 4);
     z.total = at;
     return z;
 }
 
-static Plan plan_at(const Sizes &z, const void *plan_dev)
+static Plan plan_at(const Sizes &z, int kv_heads, const void *plan_dev)
 {
     uint8_t *b = static_cast<uint8_t *>(const_cast<void *>(plan_dev));
     Plan p = z.p;
@@ -120,9 +130,10 @@ static Plan plan_at(const Sizes &z, const void *plan_dev)
     p.positions = reinterpret_cast<int32_t *>(b + z.positions);
     p.segments = reinterpret_cast<Segment *>(b + z.segments);
     p.few = reinterpret_cast<Item *>(b + z.few);
+    p.few_first = reinterpret_cast<int32_t *>(b + z.few_first);
     p.many = reinterpret_cast<Item *>(b + z.many_at);
-    p.joins_few = reinterpret_cast<Join *>(b + z.joins_few);
-    p.joins_many = reinterpret_cast<Join *>(b + z.joins_many);
+    p.joins_few = reinterpret_cast<int32_t *>(b + z.joins);
+    p.joins_many = p.joins_few + (int64_t)p.max_joins_few * kv_heads;
     return p;
 }
 
@@ -134,7 +145,7 @@ extern "C" uint64_t moe_kv_scratch_bytes(const moe_kv_step_t *step)
 {
     if (!step_ok(step)) return 0;
     const Sizes z = sizes_of(step);
-    return part_bytes(z.p.parts_few, step->kv_heads, ROWS_FEW, step->head_dim) + part_bytes(z.p.parts_many, step->kv_heads, ROWS_MANY, step->head_dim);
+    return part_bytes(z.p.parts_few, step->kv_heads, ROWS_FEW, step->head_dim) + part_bytes(z.p.parts_many, step->kv_heads, z.rows_many, step->head_dim);
 }
 
 extern "C" int32_t moe_kv_plan(const moe_kv_step_t *step, const moe_kv_lists_t *io, void *plan_dev, void *stream)
@@ -151,7 +162,7 @@ extern "C" int32_t moe_kv_plan(const moe_kv_step_t *step, const moe_kv_lists_t *
             if (p == q) return bad("moe_kv_plan: an output is an input");
     }
     const Sizes z = sizes_of(step);
-    PlanArgs a{*step, *io, plan_at(z, plan_dev), z.group, log2_of(step->page), target_blocks(BLOCKS_FEW, step->kv_heads), target_blocks(BLOCKS_MANY, step->kv_heads)};
+    PlanArgs a{*step, *io, plan_at(z, step->kv_heads, plan_dev), z.group, log2_of(step->page), z.p.blocks_few, target_blocks(BLOCKS_MANY, step->kv_heads), z.rows_many};
     const int R = step->n_requests, threads = R <= 64 ? 64 : R <= 256 ? 256 : PLAN_MOST_THREADS;
     const dim3 grid(2 + std::min(254, div_up(std::max(step->n_tokens, z.p.max_segments), threads)));
     const size_t lds = (size_t)R * 12;
@@ -209,7 +220,7 @@ extern "C" int32_t moe_kv_write(const moe_kv_cache_t *cache, const moe_kv_step_t
     WriteArgs a{};
     a.c = *cache;
     a.r = r;
-    a.p = plan_at(z, plan_dev);
+    a.p = plan_at(z, step->kv_heads, plan_dev);
     a.q_heads = step->q_heads;
     a.n_tokens = step->n_tokens;
     a.kv_blocks = z.p.max_segments * cache->kv_heads * 2;
@@ -238,12 +249,20 @@ extern "C" int32_t moe_kv_write(const moe_kv_cache_t *cache, const moe_kv_step_t
 }
 
 template <int DTYPE, int FMT>
-static void launch_attend(const AttendArgs &a, int D, dim3 grid, hipStream_t s)
+static void launch_attend(const AttendArgs &a, int D, bool decode, dim3 grid, hipStream_t s)
 {
+    if (decode) {
+        switch (D) {
+        case 64: hipLaunchKernelGGL((k_kv_decode<DTYPE, FMT, 64>), grid, dim3(64 * DECODE_WAVES), 0, s, a); break;
+        case 128: hipLaunchKernelGGL((k_kv_decode<DTYPE, FMT, 128>), grid, dim3(64 * DECODE_WAVES), 0, s, a); break;
+        default: hipLaunchKernelGGL((k_kv_decode<DTYPE, FMT, 256>), grid, dim3(64 * DECODE_WAVES), 0, s, a); break;
+        }
+        return;
+    }
     switch (D) {
-    case 64: hipLaunchKernelGGL((k_kv_attend<DTYPE, FMT, 64>), grid, dim3(ATTEND_THREADS), 0, s, a); break;
-    case 128: hipLaunchKernelGGL((k_kv_attend<DTYPE, FMT, 128>), grid, dim3(ATTEND_THREADS), 0, s, a); break;
-    default: hipLaunchKernelGGL((k_kv_attend<DTYPE, FMT, 256>), grid, dim3(ATTEND_THREADS), 0, s, a); break;
+    case 64: hipLaunchKernelGGL((k_kv_attend<DTYPE, FMT, 64>), grid, dim3(64 * attend_waves(64)), 0, s, a); break;
+    case 128: hipLaunchKernelGGL((k_kv_attend<DTYPE, FMT, 128>), grid, dim3(64 * attend_waves(128)), 0, s, a); break;
+    default: hipLaunchKernelGGL((k_kv_attend<DTYPE, FMT, 256>), grid, dim3(64 * attend_waves(256)), 0, s, a); break;
     }
 }
 
@@ -269,7 +288,7 @@ extern "C" int32_t moe_kv_attend(const moe_kv_cache_t *cache, const moe_kv_step_
     AttendArgs a{};
     a.c = *cache;
     a.q = q;
-    a.p = plan_at(z, plan_dev);
+    a.p = plan_at(z, step->kv_heads, plan_dev);
     a.table = block_table;
     a.part_few = static_cast<float *>(scratch);
     a.part_many = scratch ? reinterpret_cast<float *>(static_cast<uint8_t *>(scratch) + part_bytes(z.p.parts_few, cache->kv_heads, ROWS_FEW, D)) : nullptr;
@@ -277,29 +296,21 @@ extern "C" int32_t moe_kv_attend(const moe_kv_cache_t *cache, const moe_kv_step_
     a.max_blocks = step->max_blocks;
     a.causal = step->causal;
     a.window = step->window;
+    a.per_group = 1.f / z.group;
     a.sub_shift = log2_of(cache->page / SUB);
     a.vec_q = rows16(q.q, q.q_stride);
     a.vec_out = rows16(q.out, q.out_stride);
-    const int64_t many = (int64_t)z.p.max_many * cache->kv_heads, blocks = many + (int64_t)z.p.max_few * cache->kv_heads;
+    const int64_t many = (int64_t)z.p.max_many * cache->kv_heads, blocks = many + (int64_t)z.p.blocks_few * cache->kv_heads;
     if (blocks > 0x7FFFFFFF) return bad("moe_kv_attend: too many blocks");
     a.many_blocks = (int32_t)many;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const dim3 grid((unsigned)blocks);
     if (q.dtype == MOE_KV_F16) {
-        if (cache->format == MOE_KV_E4M3) launch_attend<MOE_KV_F16, MOE_KV_E4M3>(a, D, grid, s);
-        else launch_attend<MOE_KV_F16, MOE_KV_INT8>(a, D, grid, s);
+        if (cache->format == MOE_KV_E4M3) launch_attend<MOE_KV_F16, MOE_KV_E4M3>(a, D, z.decode, grid, s);
+        else launch_attend<MOE_KV_F16, MOE_KV_INT8>(a, D, z.decode, grid, s);
     } else {
-        if (cache->format == MOE_KV_E4M3) launch_attend<MOE_KV_BF16, MOE_KV_E4M3>(a, D, grid, s);
-        else launch_attend<MOE_KV_BF16, MOE_KV_INT8>(a, D, grid, s);
-    }
-    for (int m = 0; m < 2; ++m) {
-        const int joins = m ? z.p.max_joins_many : z.p.max_joins_few;
-        if (!joins) continue;
-        const int tile = m ? ROWS_MANY : ROWS_FEW;
-        const int rows = (int)std::min<int64_t>(tile, (int64_t)z.new_most * z.group), chunks = div_up(rows, JOIN_ROWS);
-        const dim3 g((unsigned)((int64_t)joins * cache->kv_heads * chunks));
-        if (q.dtype == MOE_KV_F16) hipLaunchKernelGGL((k_kv_join<MOE_KV_F16>), g, dim3(JOIN_THREADS), 0, s, a, m, tile, chunks);
-        else hipLaunchKernelGGL((k_kv_join<MOE_KV_BF16>), g, dim3(JOIN_THREADS), 0, s, a, m, tile, chunks);
+        if (cache->format == MOE_KV_E4M3) launch_attend<MOE_KV_BF16, MOE_KV_E4M3>(a, D, z.decode, grid, s);
+        else launch_attend<MOE_KV_BF16, MOE_KV_INT8>(a, D, z.decode, grid, s);
     }
     return launched("moe_kv_attend");
 }

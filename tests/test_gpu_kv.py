@@ -319,7 +319,7 @@ def fill(pool, lens, codes_only=False, scales="powers"):
                 pool.cache.v.view(torch.uint8)[pid, :, t // 16, :, t % 16] = 0x7F
 
 
-def check_attend(pool, step, q, out, lse, lens, new, scale, rows=None, dead=()):
+def check_attend(pool, step, q, out, lse, lens, new, scale, rows=None, heads=None):
     """Rows of requests with `lens` cached tokens in all, the last `new` of them the step's."""
     at = 0
     g = pool.q_heads // pool.kv_heads
@@ -329,7 +329,7 @@ def check_attend(pool, step, q, out, lse, lens, new, scale, rows=None, dead=()):
         pick = list(pick)
         if pick:
             ids = [max(0, int(i)) for i in pool.table[r, :-(-n // pool.page)].tolist()]
-            for h in range(pool.kv_heads):
+            for h in heads or range(pool.kv_heads):
                 k = R.cache_values(pool.cache.k, pool.cache.k_scale, pool.fmt, False, ids, h)
                 v = R.cache_values(pool.cache.v, pool.cache.v_scale, pool.fmt, True, ids, h)
                 k[n:] = 0
@@ -378,13 +378,21 @@ ATTEND = [
     dict(lens=[900, 60], new=[1, 1], dim=128, page=16, scales="wide"),
     dict(lens=[900, 60], new=[90, 1], dim=64, page=16, scales="wide", dtype=torch.bfloat16, fmt="int8"),
     dict(lens=[300, 600], new=[1, 200], dim=128, page=32, scales="any"),
+    # so many heads that a block has more steps than it knows the places of at a time
+    dict(lens=[30000, 40], new=[1, 1], dim=64, page=64, kv_heads=128, q_heads=128, heads=[0, 77, 127]),
+    dict(lens=[30000, 40], new=[20, 17], dim=64, page=64, kv_heads=128, q_heads=128, heads=[5, 127], fmt="int8"),
+    dict(lens=[30000, 200], new=[70, 100], dim=64, page=64, kv_heads=128, q_heads=128, heads=[0, 126], dtype=torch.bfloat16),
+    # many requests whose ends lie in the middle of blocks, some with nothing to do
+    dict(lens=[37 * i % 701 + 1 for i in range(150)], new=[(i * 7) % 4 and 1 for i in range(150)], dim=64, page=16, q_heads=4, kv_heads=4, heads=[2]),
+    dict(lens=[137 * i % 1701 + 9 for i in range(60)], new=[(i * 5) % 9 for i in range(60)], dim=128, page=32, q_heads=8, kv_heads=2, heads=[1], fmt="int8"),
+    dict(lens=[1037 * i % 9001 + 60 for i in range(20)], new=[1 if i % 3 else 50 for i in range(20)], dim=64, page=128, q_heads=4, kv_heads=2, heads=[0]),
 ]
 
 
-@pytest.mark.parametrize("case", ATTEND, ids=lambda c: "-".join(str(v).replace("torch.", "").replace(" ", "") for v in c.values()))
+@pytest.mark.parametrize("case", ATTEND, ids=lambda c: "-".join(str(v).replace("torch.", "").replace(" ", "")[:40] for v in c.values()))
 def test_attend(case):
     case = dict(case)
-    lens, new, scales = case.pop("lens"), case.pop("new"), case.pop("scales", "powers")
+    lens, new, scales, heads = case.pop("lens"), case.pop("new"), case.pop("scales", "powers"), case.pop("heads", None)
     page = case.setdefault("page", 64)
     p = Pool(len(lens), -(-max(lens) // page) + 1, seed=sum(lens), **case)
     fill(p, lens, scales=scales)
@@ -400,7 +408,7 @@ def test_attend(case):
     s.scratch, fence = fenced(max(16, s.scratch_bytes))
     out, lse = paged.attend(p.cache, s, q, scale, out=out, with_lse=True)
     assert (out[-1] == 7).all() and (fence == 0x5A).all()       # the last row is no request's
-    check_attend(p, s, q, out, lse, lens, new, scale, rows=6)
+    check_attend(p, s, q, out, lse, lens, new, scale, rows=6, heads=heads)
     again, lse2 = paged.attend(p.cache, s, q, scale, with_lse=True)
     assert torch.equal(again[:-1], out[:-1]) and torch.equal(lse2[:-1], lse[:-1])
 

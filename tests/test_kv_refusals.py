@@ -73,12 +73,17 @@ def test_bad_steps(k):
 
 
 def test_sizes():
-    assert B.moe_kv_plan_bytes(step()) % 64 == 0 and B.moe_kv_plan_bytes(step()) > 0
+    for page, blocks, new, n in ((16, 16, 4, 8), (16, 64, 4, 8), (128, 1024, 4, 8), (64, 4096, 512, 4096)):
+        s = step(page=page, max_blocks=blocks, max_new=new, n_tokens=n)
+        # row positions, at least, and as much again for every bound that grows
+        assert B.moe_kv_plan_bytes(s) % 64 == 0 and B.moe_kv_plan_bytes(s) >= 4 * n
+        more = step(page=page, max_blocks=blocks, max_new=new, n_tokens=2 * n, n_requests=4)
+        assert B.moe_kv_plan_bytes(more) >= B.moe_kv_plan_bytes(s) + 4 * n
     assert B.moe_kv_scratch_bytes(step()) == 0                              # 256 tokens at most: nothing is split
-    few = B.moe_kv_scratch_bytes(step(max_blocks=17))
-    assert few == 2 * 512 * 2 * 32 * 66 * 4                                 # two parts for each of 512 blocks a head, 32 rows of 64 + 2
-    assert B.moe_kv_scratch_bytes(step(max_blocks=33, max_new=9, n_tokens=9)) == few + 2 * 256 * 2 * 128 * 66 * 4
-    assert B.moe_kv_plan_bytes(step(n_requests=4096, n_tokens=1048576, max_new=1048576, q_heads=1024)) > 32 * (1048576 * 512 // 128)
+    few = B.moe_kv_scratch_bytes(step(max_blocks=1024))
+    many = B.moe_kv_scratch_bytes(step(max_blocks=1024, max_new=64, n_tokens=64))
+    assert 0 < few < many and few % (2 * 32 * 66 * 4) == 0                  # parts of two heads, 32 rows of 64 + 2 numbers
+    assert B.moe_kv_plan_bytes(step(n_requests=4096, n_tokens=1048576, max_new=1048576, q_heads=1024)) > 32 * (1048576 * 512 // 256)
 
 
 @pytest.mark.parametrize("k", [dict(n_pages=0), dict(page=17), dict(kv_heads=0), dict(head_dim=80), dict(format=2), dict(format=-1), dict(reserved=3), dict(k=None), dict(v=None),
@@ -124,7 +129,7 @@ def test_bad_queries(k):
 
 
 def test_scratch_too_small():
-    s = step(max_blocks=64)
+    s = step(max_blocks=1024)
     n = B.moe_kv_scratch_bytes(s)
     for p, b in ((P, n - 1), (None, n), (P + 8, n)):
         refused(B.moe_kv_attend, cache(), s, P, P, query(), p, b, 0, code=B.MOE_ENOMEM)
