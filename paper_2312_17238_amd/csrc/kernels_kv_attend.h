@@ -171,30 +171,54 @@ __device__ __forceinline__ float max_halves(float x)
     return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
 }
 
-// One step: 32 cached tokens against 32 rows.  k, v: the lane's pieces of the two tiles.  sc: scale log2(e) ks of the lane's
-// sub-block, lv: log2 vs, iv: 1 / vs.  edge: some row does not see some token of the step.
-template <int FMT, int D>
-__device__ __forceinline__ void step(State<D> &s, const v8h (&q)[D / 16], const uint4 (&k)[D / 32], const uint4 (&v)[D / 32],
-                                     float sc, float lv, float iv, bool edge, int tok0, Sees see)
+// How far (in powers of two) a row's maximum may rise before its sums are scaled down to it: a new maximum is common while few
+// tokens have been seen, and scaling is 64 multiplies a lane.  Weights stay below 2^8, well within fp16.
+constexpr float RISE = 8.f;
+
+// N steps: 32 N cached tokens against 32 rows.  kf(u, i, c), vf(u, n, c): the first operands of step u, dims 16 (2 i + h) + 8 c ...
+// of the keys, tokens 8 c ... of dims 32 n ... of the values.  For the lane's sub-block of each step, sc: scale log2(e) ks, lv: log2 vs,
+// iv: 1 / vs.  edge: some row does not see some token.
+template <int D, int N, class KF, class VF>
+__device__ __forceinline__ void steps(State<D> &s, const v8h (&q)[D / 16], KF kf, VF vf, const float (&sc)[N], const float (&lv)[N], const float (&iv)[N],
+                                      bool edge, const int (&tok0)[N], Sees see)
 {
-    v16f z;
+    v16f z[N];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) z[i] = 0.f;
+    for (int u = 0; u < N; ++u)
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-        z = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes_to_half<FMT>(k[i].x, k[i].y), q[2 * i], z, 0, 0, 0);
-        z = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes_to_half<FMT>(k[i].z, k[i].w), q[2 * i + 1], z, 0, 0, 0);
+        for (int i = 0; i < 16; ++i) z[u][i] = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int u = 0; u < N; ++u) z[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf(u, i, c), q[2 * i + c], z[u], 0, 0, 0);
+    if constexpr (N == 2) {
+        // six operands ahead of the matrix instruction that takes them: left alone, the compiler keeps two and waits for LDS
+        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+        for (int i = 0; i < D / 8 - 6; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
     }
     if (edge) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) z[i] = tok0 + i >= see.lo && tok0 + i < see.hi ? z[i] : -INFINITY;
-    }
-    float top = z[0];
+        for (int u = 0; u < N; ++u)
 #pragma unroll
-    for (int i = 1; i < 16; ++i) top = fmaxf(top, z[i]);
-    float t = fmaf(top, sc, lv);
+            for (int i = 0; i < 16; ++i) z[u][i] = tok0[u] + i >= see.lo && tok0[u] + i < see.hi ? z[u][i] : -INFINITY;
+    }
+    float t = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+        float top = z[u][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, z[u][i]);
+        t = fmaxf(t, fmaf(top, sc[u], lv[u]));
+    }
     t = max_halves(t);
-    if (__any(t > s.m)) {
+    if (__any(t > s.m + RISE)) {
         const float m = fmaxf(s.m, t);
         const float f = m == -INFINITY ? 1.f : exp2f(s.m - m);
         s.l *= f;
@@ -205,27 +229,45 @@ __device__ __forceinline__ void step(State<D> &s, const v8h (&q)[D / 16], const 
         s.m = m;
         s.big = __any(fabsf(m) > 0x1p20f && fabsf(m) < INFINITY);
     }
-    const float off = lv - (s.m == -INFINITY ? 0.f : s.m);
+    const float base = s.m == -INFINITY ? 0.f : s.m;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) z[i] = fmaf(z[i], sc, off);
-    // m is a rounded t, these are not: beyond 2^20 the difference shows as a weight above 1, at 2^28 one that fp16 does not hold
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) z[u][i] = fmaf(z[u][i], sc[u], lv[u] - base);
+    // m is a rounded t, these are not: beyond 2^20 the difference shows in a weight, at 2^28 as one that fp16 does not hold
     if (s.big) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) z[i] = z[i] > 0.f ? 0.f : z[i];
-    }
-    v8h p[2];
-    float sum = 0.f;
+        for (int u = 0; u < N; ++u)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const float e = __builtin_amdgcn_exp2f(z[i]);
-        sum += e;
-        p[i / 8][i % 8] = (_Float16)e;
+            for (int i = 0; i < 16; ++i) z[u][i] = z[u][i] > RISE ? RISE : z[u][i];
     }
-    s.l = fmaf(sum, iv, s.l);
 #pragma unroll
-    for (int n = 0; n < D / 32; ++n) {
-        s.o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes_to_half<FMT>(v[n].x, v[n].y), p[0], s.o[n], 0, 0, 0);
-        s.o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes_to_half<FMT>(v[n].z, v[n].w), p[1], s.o[n], 0, 0, 0);
+    for (int u = 0; u < N; ++u) {
+        v8h p[2];
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float e = __builtin_amdgcn_exp2f(z[u][i]);
+            sum += e;
+            p[i / 8][i % 8] = (_Float16)e;
+        }
+        s.l = fmaf(sum, iv[u], s.l);
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) s.o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf(u, n, c), p[c], s.o[n], 0, 0, 0);
+    }
+    if constexpr (N == 2) {
+        // the second step's exponentials beside the first one's products
+        constexpr int M = D / 8;
+        __builtin_amdgcn_sched_group_barrier(0x100, 6, 1);
+        __builtin_amdgcn_sched_group_barrier(0x400, 16, 1);
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+            if (i < M - 6) __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+            if (i < M / 2) __builtin_amdgcn_sched_group_barrier(0x400, 32 / M, 1);
+        }
     }
 }
 
@@ -470,7 +512,9 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, const Item &it, 
 #pragma unroll
                 for (int i = 0; i < D / 32; ++i) vv[i] = keep_bytes(vv[i], lo, hi);
             }
-            step<FMT, D>(s, q, kk, vv, factor * ks, __builtin_amdgcn_logf(vs), __builtin_amdgcn_rcpf(vs), edge, tok0, mask);
+            steps<D, 1>(s, q, [&](int, int i, int c) { return c ? codes_to_half<FMT>(kk[i].z, kk[i].w) : codes_to_half<FMT>(kk[i].x, kk[i].y); },
+                        [&](int, int i, int c) { return c ? codes_to_half<FMT>(vv[i].z, vv[i].w) : codes_to_half<FMT>(vv[i].x, vv[i].y); },
+                        {factor * ks}, {__builtin_amdgcn_logf(vs)}, {__builtin_amdgcn_rcpf(vs)}, edge, {tok0}, mask);
         };
         // No branch around a load (past the end the last step is requested again): the compiler then waits for the step it
         // needs alone, with the next one's loads in flight.
@@ -542,11 +586,13 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, const Item &it, 
     if (!whole && all_parts_done(a.p.joins_few + it.join * heads + head, it.parts, sh.join)) join_parts<DTYPE, D>(a, it, head, a.part_few, ml, ROWS_FEW, sh.join);
 }
 
-// ---- tiles of 32 rows a wave: every wave has its own, all waves share the block's steps through LDS, two steps at a time
+// ---- tiles of 32 rows a wave: every wave has its own, all waves share the block's steps through LDS, two at a time.  The codes
+// become fp16 numbers once, on their way into LDS: left to the waves, the conversion was a third of their vector instructions, which
+// are the bound here (MEASURED_MANY).
 template <int D>
 struct ManyShared {
     static constexpr int PLACES = 256;      // sub-blocks whose places are known at a time
-    uint4 k[2][4 * D], v[2][4 * D];         // [buffer][sub-block of the two steps][pieces]
+    v8h k[2][2][4 * D], v[2][2][4 * D];     // [buffer][half of a piece][sub-block of the two steps][piece of 16 codes]
     Place place[PLACES];
     JoinShared join;
 };
@@ -564,11 +610,11 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const Item &it,
     const Sees see = sees(a, it, row);
     const float factor = a.q.scale * LOG2E * unit;
     const int pos_a = it.ctx + __builtin_amdgcn_readlane(row.tok, 0), pos_z = it.ctx + __builtin_amdgcn_readlane(row.tok, max(0, min(31, rows - 1 - row0)));
-    const int end = it.ctx + it.n_new;
+    const int end = it.ctx + it.n_new, part_hi = min(end, it.kt1 * KT);
     const int any_lo = a.window > 0 ? max(0, pos_a + 1 - a.window) : 0, any_hi = row0 >= rows ? 0 : a.causal ? pos_z + 1 : end;
-    const int all_lo = a.window > 0 ? max(0, pos_z + 1 - a.window) : 0, all_hi = a.causal ? pos_a + 1 : end;
+    const int all_lo = a.window > 0 ? max(0, pos_z + 1 - a.window) : 0, all_hi = min(part_hi, a.causal ? pos_a + 1 : end);
     // values before this one may lie in pages that the request has given back
-    const int tile_lo = a.window > 0 ? max(0, it.ctx + it.tile * ROWS / a.group + 1 - a.window) : 0;
+    const int tile_lo = a.window > 0 ? max(0, it.ctx + tile0 / a.group + 1 - a.window) : 0;
     State<D> s;
     clear(s);
 
@@ -576,64 +622,69 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const Item &it,
     const int kh = (col >> 2) & 1, ktok = 4 * (col >> 3) + (col & 3);
     const uint4 *kbase = static_cast<const uint4 *>(a.c.k), *vbase = static_cast<const uint4 *>(a.c.v);
     constexpr int PER = div_up(4 * D, THREADS);     // pieces of 16 bytes of a thread: two steps hold 4 D of each kind
-    const bool loads = 4 * D >= THREADS || tid < 4 * D;
     for (int batch = it.kt0; batch < it.kt1; batch += ManyShared<D>::PLACES / 2) {
-        const int last = min(it.kt1, batch + ManyShared<D>::PLACES / 2);
+        const int last = min(it.kt1, batch + ManyShared<D>::PLACES / 2), places = 2 * (last - batch);
         __syncthreads();
-        for (int i = tid; i < 2 * (last - batch) + 2; i += THREADS)
-            if (i < ManyShared<D>::PLACES) sh.place[i] = place_of(a, it, head, 2 * batch + i, end);
+        for (int i = tid; i < places; i += THREADS) sh.place[i] = place_of(a, it, head, 2 * batch + i, end);
         __syncthreads();
         uint4 rk[PER], rv[PER];
+        int id[PER];
         auto fetch = [&](int kt) {
-            if (!loads) return;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
                 const int piece = tid + i * THREADS, sb = piece / D, in = piece - sb * D;
-                const int idx = 2 * (kt - batch) + sb;
-                const int id = idx < ManyShared<D>::PLACES && kt + sb / 2 < last ? max(sh.place[idx].id, 0) : 0;
-                const int64_t at = (((int64_t)id * heads + head) * subs + ((2 * kt + sb) & (subs - 1))) * D + in;
+                id[i] = sh.place[min(2 * (kt - batch) + sb, places - 1)].id;
+                const int64_t at = (((int64_t)max(id[i], 0) * heads + head) * subs + ((2 * kt + sb) & (subs - 1))) * D + in;
                 rk[i] = kbase[at];
                 rv[i] = vbase[at];
             }
         };
-        auto put = [&](int buf) {
-            if (!loads) return;
+        auto put = [&](int kt, int buf) {
+            const bool whole = kt * KT >= tile_lo && (kt + 2) * KT <= part_hi;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                sh.k[buf][tid + i * THREADS] = rk[i];
-                sh.v[buf][tid + i * THREADS] = rv[i];
+                const int piece = tid + i * THREADS;
+                if (!whole || id[i] < 0) {          // bytes that may be anything: before the window, behind the last token, of no page
+                    const int tok0 = kt * KT + piece / D * SUB;
+                    rv[i] = keep_bytes(rv[i], tile_lo - tok0, id[i] < 0 ? 0 : part_hi - tok0);
+                }
+                sh.k[buf][0][piece] = codes_to_half<FMT>(rk[i].x, rk[i].y);
+                sh.k[buf][1][piece] = codes_to_half<FMT>(rk[i].z, rk[i].w);
+                sh.v[buf][0][piece] = codes_to_half<FMT>(rv[i].x, rv[i].y);
+                sh.v[buf][1][piece] = codes_to_half<FMT>(rv[i].z, rv[i].w);
             }
         };
         fetch(batch);
-        put(0);
+        put(batch, 0);
         __syncthreads();
         int buf = 0;
         for (int kt = batch; kt < last; kt += 2) {
             const bool more = kt + 2 < last;
-            if (more) fetch(kt + 2);
+            fetch(more ? kt + 2 : kt);              // no branch around a load
+            const int tok = kt * KT;
+            if (tok < any_hi && tok + 2 * KT > any_lo) {
+                Place pl[2];
+                float sc[2], lv[2], iv[2];
+                int tok0[2];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int tok = (kt + u) * KT;
-                if (kt + u < last && tok < any_hi && tok + KT > any_lo) {
-                    const Place pl = sh.place[2 * (kt + u - batch) + h];
-                    const bool edge = tok < all_lo || tok + KT > all_hi || __any(pl.id < 0);
-                    uint4 kk[D / 32], vv[D / 32];
-#pragma unroll
-                    for (int i = 0; i < D / 32; ++i) {
-                        kk[i] = sh.k[buf][(2 * u + kh) * D + (2 * i + h) * 16 + ktok];
-                        vv[i] = sh.v[buf][(2 * u + h) * D + i * 32 + col];
-                    }
-                    Sees mask = see;
-                    if (edge) {
-                        if (pl.id < 0) mask.hi = 0;
-                        const int tok0 = tok + SUB * h, lo = tile_lo - tok0, hi = pl.id < 0 ? 0 : end - tok0;
-#pragma unroll
-                        for (int i = 0; i < D / 32; ++i) vv[i] = keep_bytes(vv[i], lo, hi);
-                    }
-                    step<FMT, D>(s, q, kk, vv, factor * pl.ks, __builtin_amdgcn_logf(pl.vs), __builtin_amdgcn_rcpf(pl.vs), edge, tok + SUB * h, mask);
+                for (int u = 0; u < 2; ++u) {
+                    pl[u] = sh.place[min(2 * (kt + u - batch) + h, places - 1)];
+                    sc[u] = factor * pl[u].ks;
+                    lv[u] = __builtin_amdgcn_logf(pl[u].vs);
+                    iv[u] = __builtin_amdgcn_rcpf(pl[u].vs);
+                    tok0[u] = tok + u * KT + SUB * h;
                 }
+                const bool edge = tok < all_lo || tok + 2 * KT > all_hi || __any(pl[0].id < 0 || pl[1].id < 0);
+                Sees mask{see.lo, min(see.hi, part_hi)};
+                // a sub-block that is nowhere: its tokens as if behind all that the row sees
+                if (edge) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) tok0[u] = pl[u].id < 0 ? 0x40000000 : tok0[u];
+                }
+                steps<D, 2>(s, q, [&](int u, int i, int c) { return sh.k[buf][c][(2 * u + kh) * D + (2 * i + h) * 16 + ktok]; },
+                            [&](int u, int n, int c) { return sh.v[buf][c][(2 * u + h) * D + n * 32 + col]; }, sc, lv, iv, edge, tok0, mask);
             }
-            if (more) put(buf ^ 1);
+            if (more) put(kt + 2, buf ^ 1);
             __syncthreads();
             buf ^= 1;
         }

@@ -22,7 +22,8 @@ constexpr int FEW_MOST = 64;       // requests of up to this many rows are made 
 constexpr int COMPUTE_UNITS = 256;
 constexpr int BLOCKS_FEW = 2 * COMPUTE_UNITS;    // blocks that the cached tokens of small requests are shared out to: two a compute unit
 constexpr int BLOCKS_MANY = 512;
-constexpr int MIN_KT_FEW = 32;     // steps of a block at least
+constexpr int MIN_KT_FEW = 16;     // steps of a block at least
+constexpr int SPLIT_STEPS = 32;    // what joining a tile's parts costs, in steps of a block
 constexpr int MIN_KT_MANY = 16;
 
 // A piece of work, for each kv head: rows [tile * ROWS, ...) of a request against the cached tokens [kt0, kt1) * KT.

@@ -210,7 +210,7 @@ struct Decode {
 #pragma unroll
                 for (int t = 1; t < 4; ++t) top = fmaxf(fmaxf(top, fmaxf(z[t][0], z[t][1])), fmaxf(z[t][2], z[t][3]));
                 const float s = max_quarters(fmaf(top, sc, lv));
-                if (__any(s > m)) {
+                if (__any(s > m + RISE)) {
                     const float up = fmaxf(m, s), f = up == -INFINITY ? 1.f : exp2f(m - up);
                     l *= f;
 #pragma unroll
@@ -223,11 +223,11 @@ struct Decode {
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) z[t][i] = fmaf(z[t][i], sc, off);
-                if (big) {      // as in step()
+                if (big) {      // as in steps()
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) z[t][i] = z[t][i] > 0.f ? 0.f : z[t][i];
+                        for (int i = 0; i < 4; ++i) z[t][i] = z[t][i] > RISE ? RISE : z[t][i];
                 }
                 v8h p[2];
                 float sum = 0.f;

@@ -76,6 +76,19 @@ __device__ __forceinline__ double block_sum(double v, double *tmp)
     return v;
 }
 
+template <int THREADS>
+__device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t *tmp)
+{
+    for (int d = 32; d > 0; d >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d));
+    if constexpr (THREADS > 64) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = v;
+        __syncthreads();
+        for (int w = 0; w < THREADS / 64; ++w) v = max(v, tmp[w]);
+    }
+    return v;
+}
+
 // first i with sums[i] > x, sums ascending; n if there is none
 __device__ __forceinline__ int first_above(const int32_t *sums, int n, int x)
 {
@@ -188,7 +201,9 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
         block_scan<THREADS>(used, tmp, &total);
         // Tiles of 32 rows, one after the other on a line of steps (a tile that sees nothing takes one step of it): every
         // block gets a piece of the line of the same length, whatever tiles begin and end in it.  A tile that lies in several
-        // pieces is joined from its parts.  Sums stay below 2^32: 8192 tiles of less than 2^19 steps.
+        // pieces is joined from its parts.  Where there is a block for every tile and the longest tile is not much longer than such a piece
+        // each block gets a tile instead: to join parts costs what SPLIT_STEPS steps cost.
+        // Sums stay below 2^32: 8192 tiles of less than 2^19 steps.
         auto tiles_of = [&](int i) {
             const int rows = now[i] * a.group;
             return rows > FEW_MOST || st[i] == MOE_KV_BAD_SIZE ? 0 : div_up(rows, ROWS_FEW);
@@ -198,7 +213,7 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
             if (!st[i]) key_steps(s, ctx[i], now[i], tile * ROWS_FEW / a.group, (min((tile + 1) * ROWS_FEW, now[i] * a.group) - 1) / a.group, it.kt0, it.kt1);
             return it;
         };
-        uint32_t steps = 0, line;
+        uint32_t steps = 0, line, longest = 0, tiles = 0, all_tiles;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int r = r0 + i;
@@ -210,6 +225,8 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
             for (int t = 0; t < tiles_of(i); ++t) {
                 const Item it = item_of(i, t);
                 steps += max(1, it.kt1 - it.kt0);
+                longest = max(longest, (uint32_t)(it.kt1 - it.kt0));
+                ++tiles;
             }
         }
         if (tid == 0) {
@@ -217,7 +234,24 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
             a.io.free_left[0] = free_n - (int)total;
         }
         const uint32_t start = block_scan<THREADS>(steps, tmp, &line) - steps;
-        const uint32_t chunk = max((uint32_t)MIN_KT_FEW, (line + a.target_few - 1) / a.target_few);
+        const uint32_t tile0 = block_scan<THREADS>(tiles, tmp, &all_tiles) - tiles;
+        const uint32_t even = (line + a.target_few - 1) / a.target_few;
+        const uint32_t chunk = all_tiles <= (uint32_t)a.target_few ? max((uint32_t)MIN_KT_FEW, even) : max(1u, even);
+        const bool whole = block_max<THREADS>(longest, tmp) <= chunk + SPLIT_STEPS && all_tiles <= (uint32_t)a.target_few;
+        if (whole) {
+            uint32_t at = tile0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                for (int t = tiles_of(i) - 1; t >= 0; --t, ++at) {
+                    a.p.few[at] = item_of(i, t);
+                    a.p.few_first[at] = (int)at;
+                }
+            if (tid == 0) {
+                a.p.head->few_blocks = (int)all_tiles;
+                a.p.few_first[all_tiles] = (int)all_tiles;
+            }
+            return;
+        }
         uint32_t items = 0, split = 0, pos = start;      // split: joins << 16 | parts
 #pragma unroll
         for (int i = 0; i < PER; ++i)

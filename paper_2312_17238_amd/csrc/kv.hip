@@ -98,7 +98,7 @@ static Sizes sizes_of(const moe_kv_step_t *s)
     const int tiles_few = (int)std::min<int64_t>((int64_t)std::min(R, T) * div_up((int)std::min<int64_t>(FEW_MOST, (int64_t)z.new_most * z.group), ROWS_FEW),
                                                  (int64_t)T * z.group / ROWS_FEW + std::min(R, T));
     const bool split_few = (int64_t)tiles_few * steps > MIN_KT_FEW;     // more than one block
-    p.blocks_few = split_few ? tf : 1;
+    p.blocks_few = split_few ? tf : tiles_few;
     p.max_few = tiles_few + p.blocks_few;
     const int tiles = z.many ? (int)((int64_t)T * z.group / z.rows_many) + std::min(R, T) : 0;
     p.max_many = tiles + (split_many ? tm : 0);
@@ -223,19 +223,22 @@ extern "C" int32_t moe_kv_write(const moe_kv_cache_t *cache, const moe_kv_step_t
     a.p = plan_at(z, step->kv_heads, plan_dev);
     a.q_heads = step->q_heads;
     a.n_tokens = step->n_tokens;
-    a.kv_blocks = z.p.max_segments * cache->kv_heads * 2;
-    a.q_tokens = step->n_tokens >= 2048 ? 4 : 1;
+    const int per_pass = WRITE_THREADS / (D / 8), angles = r.rot_dim / 2 * 8, most = std::min(cache->page, z.new_most);
+    a.heads = std::max(1, std::min(std::min(cache->kv_heads, WRITE_HEADS), per_pass / most));
+    a.lds_rows = std::max(most, a.heads * most);
+    a.kv_blocks = z.p.max_segments * div_up(cache->kv_heads, a.heads) * 2;
+    a.q_tokens = step->n_tokens >= 2048 ? 2 : 1;
     a.vec_q = rows16(r.q, r.q_stride);
     a.vec_k = rows16(r.k, r.k_stride);
     a.vec_v = rows16(r.v, r.v_stride);
     a.vec_qo = rows16(r.q_out, r.q_out_stride);
     // queries that neither turn nor move need no block
     const bool turn = r.rot_dim || r.eps > 0.f || r.q != r.q_out;
-    const int64_t blocks = (int64_t)z.p.max_segments * cache->kv_heads * 2 + (turn ? div_up(step->n_tokens, a.q_tokens) : 0);
+    const int64_t blocks = (int64_t)z.p.max_segments * div_up(cache->kv_heads, a.heads) * 2 + (turn ? div_up(step->n_tokens, a.q_tokens) : 0);
     if (blocks > 0x7FFFFFFF) return bad("moe_kv_write: too many blocks");
-    const int per_pass = WRITE_THREADS / (D / 8), angles = r.rot_dim / 2 * 8;
-    const size_t lds = std::max<size_t>((size_t)cache->page * (D + 16) + per_pass * angles, (size_t)a.q_tokens * angles);
-    const int iter = std::max(1, cache->page / per_pass);
+    const size_t lds = std::max<size_t>((size_t)a.lds_rows * (D + 16) + per_pass * angles, (size_t)a.q_tokens * angles);
+    int iter = 1;
+    while (iter * per_pass < a.lds_rows) iter *= 2;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const dim3 grid((unsigned)blocks);
     if (r.dtype == MOE_KV_F16) {
