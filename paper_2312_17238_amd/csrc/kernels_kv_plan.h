@@ -4,7 +4,7 @@
 // it gets), pages touched (the segments that the store works on), tiles of rows and steps over cached tokens (the attention's
 // blocks).  Up to 4096 requests are 16 KB of lengths, so every block of the launch makes the sums it needs by
 // itself, in LDS, and there is no exchange between blocks: block 0 writes what is per request and shares out the requests of
-// few rows, block 1 those of many, the others look up rows and pages with a binary search in the sums.  Latency is all there is
+// few rows, the next ones those of many, the others look up rows and pages with a binary search in the sums.  Latency is all there is
 // to it: 2048 requests with 77 thousand rows move 0.7 MB.
 #pragma once
 #include "kernels_common.h"
@@ -20,6 +20,7 @@ struct PlanArgs {
     moe_kv_lists_t io;
     Plan p;
     int32_t group, page_shift, target_few, target_many, rows_many;
+    int32_t many_blocks;    // blocks that share out the requests of many rows
 };
 
 // a + b, 2^32 - 1 at most: sums of lengths that no batch can have stay above every bound they are compared with
@@ -123,10 +124,15 @@ __device__ __forceinline__ void put_items(Item *items, Item it, int n, int item0
     it.part0 = part0;
     it.parts = n;
     it.join = join;
-    for (int p = 0; p < n; ++p) {
-        it.kt0 = lo + (int)((int64_t)len * p / n);
-        it.kt1 = lo + (int)((int64_t)len * (p + 1) / n);
-        it.part = n > 1 ? part0 + p : -1;
+    if (n == 1) {
+        it.part = -1;
+        items[item0] = it;
+        return;
+    }
+    for (uint32_t p = 0; p < (uint32_t)n; ++p) {        // less than 2^19 steps, 2^11 parts
+        it.kt0 = lo + (int)((uint32_t)len * p / (uint32_t)n);
+        it.kt1 = lo + (int)((uint32_t)len * (p + 1) / (uint32_t)n);
+        it.part = part0 + (int)p;
         items[item0 + p] = it;
     }
 }
@@ -150,11 +156,18 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
     uint32_t sum = 0, total;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
+        // no branch around the loads: they are on their way together
         const int r = r0 + i;
-        ctx[i] = now[i] = st[i] = 0;
-        if (i < per && r < R) {
-            ctx[i] = a.io.ctx_len[r];
-            now[i] = a.io.new_len[r];
+        ctx[i] = a.io.ctx_len[min(r, R - 1)];
+        now[i] = a.io.new_len[min(r, R - 1)];
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int r = r0 + i;
+        st[i] = 0;
+        if (i >= per || r >= R) {
+            ctx[i] = now[i] = 0;
+        } else {
             if (ctx[i] < 0 || now[i] < 0 || now[i] > s.max_new) st[i] = MOE_KV_BAD_SIZE;
             ctx[i] = max(ctx[i], 0);
             now[i] = min(max(now[i], 0), T + 1);
@@ -190,7 +203,8 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
         if (i < per && r < R) {
             if (need[i] > 0 && add_sat(before, need[i]) > (uint32_t)free_n) st[i] = MOE_KV_NO_PAGES;
             if (!st[i]) used += need[i];
-            need_before[r] = st[i] ? -1 : (int)min(before, 0x7FFFFFFFu);      // at most free_n where it is used
+            // pages: at most free_n where it is used; the block that shares out tiles looks up the cached tokens instead
+            need_before[r] = st[i] ? -1 : (int)blockIdx.x <= a.many_blocks ? ctx[i] : (int)min(before, 0x7FFFFFFFu);
         }
         before = add_sat(before, need[i]);
     }
@@ -204,29 +218,27 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
         // pieces is joined from its parts.  Where there is a block for every tile and the longest tile is not much longer than such a piece
         // each block gets a tile instead: to join parts costs what SPLIT_STEPS steps cost.
         // Sums stay below 2^32: 8192 tiles of less than 2^19 steps.
-        auto tiles_of = [&](int i) {
-            const int rows = now[i] * a.group;
-            return rows > FEW_MOST || st[i] == MOE_KV_BAD_SIZE ? 0 : div_up(rows, ROWS_FEW);
-        };
-        auto item_of = [&](int i, int tile) {
-            Item it{r0 + i, first[i], now[i], ctx[i], tile, 0, 0, -1, 0, 0, 0, 0};
-            if (!st[i]) key_steps(s, ctx[i], now[i], tile * ROWS_FEW / a.group, (min((tile + 1) * ROWS_FEW, now[i] * a.group) - 1) / a.group, it.kt0, it.kt1);
-            return it;
-        };
-        uint32_t steps = 0, line, longest = 0, tiles = 0, all_tiles;
+        constexpr int TILES = FEW_MOST / ROWS_FEW;
+        int tiles[PER], kt0[PER][TILES], kt1[PER][TILES];
+        uint32_t steps = 0, line, longest = 0, n_tiles = 0, all_tiles;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int r = r0 + i;
+            const int r = r0 + i, rows = now[i] * a.group;
+            tiles[i] = rows > FEW_MOST || st[i] == MOE_KV_BAD_SIZE ? 0 : div_up(rows, ROWS_FEW);
             if (i < per && r < R) {
                 a.io.row_start[r + 1] = first[i] + now[i];
                 a.io.kv_len[r] = st[i] ? ctx[i] : ctx[i] + now[i];
                 a.io.status[r] = st[i];
             }
-            for (int t = 0; t < tiles_of(i); ++t) {
-                const Item it = item_of(i, t);
-                steps += max(1, it.kt1 - it.kt0);
-                longest = max(longest, (uint32_t)(it.kt1 - it.kt0));
-                ++tiles;
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                kt0[i][t] = kt1[i][t] = 0;
+                if (t < tiles[i]) {
+                    if (!st[i]) key_steps(s, ctx[i], now[i], t * ROWS_FEW / a.group, (min((t + 1) * ROWS_FEW, rows) - 1) / a.group, kt0[i][t], kt1[i][t]);
+                    steps += max(1, kt1[i][t] - kt0[i][t]);
+                    longest = max(longest, (uint32_t)(kt1[i][t] - kt0[i][t]));
+                    ++n_tiles;
+                }
             }
         }
         if (tid == 0) {
@@ -234,7 +246,7 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
             a.io.free_left[0] = free_n - (int)total;
         }
         const uint32_t start = block_scan<THREADS>(steps, tmp, &line) - steps;
-        const uint32_t tile0 = block_scan<THREADS>(tiles, tmp, &all_tiles) - tiles;
+        const uint32_t tile0 = block_scan<THREADS>(n_tiles, tmp, &all_tiles) - n_tiles;
         const uint32_t even = (line + a.target_few - 1) / a.target_few;
         const uint32_t chunk = all_tiles <= (uint32_t)a.target_few ? max((uint32_t)MIN_KT_FEW, even) : max(1u, even);
         const bool whole = block_max<THREADS>(longest, tmp) <= chunk + SPLIT_STEPS && all_tiles <= (uint32_t)a.target_few;
@@ -242,10 +254,13 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
             uint32_t at = tile0;
 #pragma unroll
             for (int i = 0; i < PER; ++i)
-                for (int t = tiles_of(i) - 1; t >= 0; --t, ++at) {
-                    a.p.few[at] = item_of(i, t);
-                    a.p.few_first[at] = (int)at;
-                }
+#pragma unroll
+                for (int t = TILES - 1; t >= 0; --t)
+                    if (t < tiles[i]) {
+                        a.p.few[at] = Item{r0 + i, first[i], now[i], ctx[i], t, kt0[i][t], kt1[i][t], -1, 0, 1, 0, 0};
+                        a.p.few_first[at] = (int)at;
+                        ++at;
+                    }
             if (tid == 0) {
                 a.p.head->few_blocks = (int)all_tiles;
                 a.p.few_first[all_tiles] = (int)all_tiles;
@@ -253,39 +268,42 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
             return;
         }
         uint32_t items = 0, split = 0, pos = start;      // split: joins << 16 | parts
+        uint32_t b0[PER][TILES], parts[PER][TILES];
 #pragma unroll
         for (int i = 0; i < PER; ++i)
-            for (int t = 0; t < tiles_of(i); ++t) {
-                const Item it = item_of(i, t);
-                const uint32_t len = max(1, it.kt1 - it.kt0), n = (pos + len - 1) / chunk - pos / chunk + 1;
-                items += n;
-                split += n > 1 ? (1u << 16) + n : 0;
-                pos += len;
-            }
+#pragma unroll
+            for (int t = 0; t < TILES; ++t)
+                if (t < tiles[i]) {
+                    const uint32_t len = max(1, kt1[i][t] - kt0[i][t]);
+                    b0[i][t] = pos / chunk;
+                    const uint32_t n = parts[i][t] = (pos + len - 1) / chunk - b0[i][t] + 1;
+                    items += n;
+                    split += n > 1 ? (1u << 16) + n : 0;
+                    pos += len;
+                }
         uint32_t all_items, all_split;
         uint32_t item0 = block_scan<THREADS>(items, tmp, &all_items) - items, split0 = block_scan<THREADS>(split, tmp, &all_split) - split;
         pos = start;
 #pragma unroll
         for (int i = 0; i < PER; ++i)
-            for (int t = 0; t < tiles_of(i); ++t) {
-                Item it = item_of(i, t);
-                const int len = it.kt1 - it.kt0, kt0 = it.kt0;
-                const uint32_t b0 = pos / chunk, n = (pos + max(1, len) - 1) / chunk - b0 + 1;
-                it.part0 = split0 & 0xFFFF;
-                it.parts = n;
-                it.join = split0 >> 16;
-                for (uint32_t p = 0; p < n; ++p) {
-                    const int at = (int)((b0 + p) * chunk - pos);        // where the block's piece begins, from the tile's first step
-                    it.kt0 = kt0 + max(0, at);
-                    it.kt1 = kt0 + min(len, at + (int)chunk);
-                    it.part = n > 1 ? it.part0 + p : -1;
-                    a.p.few[item0 + p] = it;
-                    if (at >= 0) a.p.few_first[b0 + p] = item0 + p;      // the block's first item
+#pragma unroll
+            for (int t = 0; t < TILES; ++t)
+                if (t < tiles[i]) {
+                    const int len = kt1[i][t] - kt0[i][t];
+                    const uint32_t n = parts[i][t];
+                    Item it{r0 + i, first[i], now[i], ctx[i], t, 0, 0, -1, (int)(split0 & 0xFFFF), (int)n, (int)(split0 >> 16), 0};
+                    for (uint32_t p = 0; p < n; ++p) {
+                        const int at = (int)((b0[i][t] + p) * chunk - pos);      // where the block's piece begins, from the tile's first step
+                        it.kt0 = kt0[i][t] + max(0, at);
+                        it.kt1 = kt0[i][t] + min(len, at + (int)chunk);
+                        it.part = n > 1 ? it.part0 + (int)p : -1;
+                        a.p.few[item0 + p] = it;
+                        if (at >= 0) a.p.few_first[b0[i][t] + p] = item0 + p;    // the block's first item
+                    }
+                    item0 += n;
+                    split0 += n > 1 ? (1u << 16) + n : 0;
+                    pos += max(1, len);
                 }
-                item0 += n;
-                split0 += n > 1 ? (1u << 16) + n : 0;
-                pos += max(1, len);
-            }
         if (tid == 0) {
             const uint32_t blocks = (line + chunk - 1) / chunk;
             a.p.head->few_blocks = (int)blocks;
@@ -293,7 +311,7 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
         }
         return;
     }
-    if (role == 1) {
+    if (role <= a.many_blocks) {
         // Tiles of the other requests.  A request of a bad size has none: it may have more rows than the lists
         // are made for.
         auto tiles_of = [&](int i) {
@@ -305,7 +323,7 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
         for (int i = 0; i < PER; ++i) units += tiles_of(i);
         uint32_t unit_at = block_scan<THREADS>(units, tmp, &n_units) - units;
         if (n_units == 0) {
-            if (tid == 0) a.p.head->many = 0;
+            if (tid == 0 && role == 1) a.p.head->many = 0;
             return;
         }
 #pragma unroll
@@ -320,19 +338,32 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
             it.req = r;
             it.row0 = begin;
             it.n_new = n;
-            it.ctx = max(a.io.ctx_len[r], 0);
+            it.ctx = max(need_before[r], 0);
             it.tile = sums[r] - 1 - u;                   // the last rows see most: they go first
             it.kt0 = it.kt1 = 0;                         // turned down: nothing to attend to
             if (need_before[r] >= 0)
                 key_steps(s, it.ctx, n, it.tile * a.rows_many / a.group, (min((it.tile + 1) * a.rows_many, n * a.group) - 1) / a.group, it.kt0, it.kt1);
         };
         double steps = 0.0;
+        uint32_t longest = 0;
         for (int u = tid; u < (int)n_units; u += THREADS) {
             Item it{};
             unit(u, it);
             steps += it.kt1 - it.kt0;
+            longest = max(longest, (uint32_t)(it.kt1 - it.kt0));
         }
         const int chunk = share(block_sum<THREADS>(steps, tmp_d), a.target_many, MIN_KT_MANY);
+        if (block_max<THREADS>(longest, tmp) <= (uint32_t)chunk) {
+            // no tile is split: items are tiles, and the blocks of this role write them together
+            for (int u = (role - 1) * THREADS + tid; u < (int)n_units; u += a.many_blocks * THREADS) {
+                Item it{};
+                unit(u, it);
+                put_items(a.p.many, it, 1, u, 0, 0);
+            }
+            if (tid == 0 && role == 1) a.p.head->many = (int)n_units;
+            return;
+        }
+        if (role > 1) return;
         uint32_t items = 0, split = 0;
         for (int base = 0; base < (int)n_units; base += THREADS) {
             Item it{};
@@ -373,7 +404,7 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
         if (blk < held) return a.io.block_table[(int64_t)r * s.max_blocks + blk];
         return a.io.free_pages[free_n - 1 - (need_before[r] + blk - held)];
     };
-    const int worker = role - 2, workers = gridDim.x - 2;
+    const int worker = role - 1 - a.many_blocks, workers = gridDim.x - 1 - a.many_blocks;
     for (int i = worker * THREADS + tid; i < (a.p.max_joins_few + a.p.max_joins_many) * s.kv_heads; i += workers * THREADS) a.p.joins_few[i] = 0;
     for (int t = worker * THREADS + tid; t < T; t += workers * THREADS) {
         const int r = first_above(row_end, R, t);

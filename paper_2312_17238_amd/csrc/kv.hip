@@ -162,9 +162,9 @@ extern "C" int32_t moe_kv_plan(const moe_kv_step_t *step, const moe_kv_lists_t *
             if (p == q) return bad("moe_kv_plan: an output is an input");
     }
     const Sizes z = sizes_of(step);
-    PlanArgs a{*step, *io, plan_at(z, step->kv_heads, plan_dev), z.group, log2_of(step->page), z.p.blocks_few, target_blocks(BLOCKS_MANY, step->kv_heads), z.rows_many};
+    PlanArgs a{*step, *io, plan_at(z, step->kv_heads, plan_dev), z.group, log2_of(step->page), z.p.blocks_few, target_blocks(BLOCKS_MANY, step->kv_heads), z.rows_many, std::min(8, std::max(1, div_up(z.p.max_many, PLAN_MOST_THREADS)))};
     const int R = step->n_requests, threads = R <= 64 ? 64 : R <= 256 ? 256 : PLAN_MOST_THREADS;
-    const dim3 grid(2 + std::min(254, div_up(std::max(step->n_tokens, z.p.max_segments), threads)));
+    const dim3 grid(1 + a.many_blocks + std::min(240, div_up(std::max(step->n_tokens, z.p.max_segments), threads)));
     const size_t lds = (size_t)R * 12;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (threads == 64) hipLaunchKernelGGL((k_kv_plan<64, 1>), grid, dim3(64), lds, st, a);
