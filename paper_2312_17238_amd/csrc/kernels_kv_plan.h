@@ -103,18 +103,19 @@ __device__ __forceinline__ int first_above(const int32_t *sums, int n, int x)
 }
 
 // Steps [kt0, kt1) over the cached tokens that rows of a request see, tokens [tok_first, tok_last].
-__device__ __forceinline__ void key_steps(const moe_kv_step_t &s, int ctx, int n_new, int tok_first, int tok_last, int &kt0, int &kt1)
+__host__ __device__ __forceinline__ void key_steps(const moe_kv_step_t &s, int ctx, int n_new, int tok_first, int tok_last, int &kt0, int &kt1)
 {
-    const int hi = s.causal ? ctx + tok_last + 1 : ctx + n_new;
-    const int lo = s.window > 0 ? max(0, ctx + tok_first + 1 - s.window) : 0;
+    const int hi = s.causal ? ctx + tok_last + 1 : ctx + n_new, first = ctx + tok_first + 1 - s.window;
+    const int lo = s.window > 0 && first > 0 ? first : 0;
     kt0 = lo / KT;
     kt1 = (hi + KT - 1) / KT;
 }
 
 // The steps of a block where `all` steps are shared out to `target` blocks of at least `least`.
-__device__ __forceinline__ int share(double all, int target, int least)
+__host__ __device__ __forceinline__ int share(double all, int target, int least)
 {
-    return max(least, (int)(((int64_t)all + target - 1) / target));
+    const int even = (int)(((int64_t)all + target - 1) / target);
+    return even > least ? even : least;
 }
 
 // Writes the items of one tile, in as many parts as `n`.
