@@ -252,10 +252,11 @@ __device__ __forceinline__ void steps(State<D> &s, const v8h (&q)[D / 16], KF kf
             p[i / 8][i % 8] = (_Float16)e;
         }
         s.l = fmaf(sum, iv[u], s.l);
+        // neighbouring instructions into different outputs: one into the same waits for it
 #pragma unroll
-        for (int n = 0; n < D / 32; ++n)
+        for (int c = 0; c < 2; ++c)
 #pragma unroll
-            for (int c = 0; c < 2; ++c) s.o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf(u, n, c), p[c], s.o[n], 0, 0, 0);
+            for (int n = 0; n < D / 32; ++n) s.o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf(u, n, c), p[c], s.o[n], 0, 0, 0);
     }
     if constexpr (N == 2) {
         // the second step's exponentials beside the first one's products
@@ -290,6 +291,19 @@ __device__ __forceinline__ Place place_of(const AttendArgs &a, const Item &it, i
         }
     }
     return p;
+}
+
+// The same as the steps use it: in units of sub-blocks of all pages and heads, ks = 0 for nowhere, log2 vs, 1 / vs.
+struct __align__(16) Spot {
+    uint32_t at;
+    float ks, lv, iv;
+};
+
+__device__ __forceinline__ Spot spot_of(const AttendArgs &a, const Item &it, int head, int sub_block, int end_tok)
+{
+    const Place p = place_of(a, it, head, sub_block, end_tok);
+    const uint32_t page = (uint32_t)max(p.id, 0) * a.c.kv_heads + head;
+    return {(page << a.sub_shift) + (sub_block & ((1 << a.sub_shift) - 1)), p.id < 0 ? 0.f : p.ks, __builtin_amdgcn_logf(p.vs), __builtin_amdgcn_rcpf(p.vs)};
 }
 
 // Writes two or four neighbouring numbers of an output row.
@@ -593,7 +607,7 @@ template <int D>
 struct ManyShared {
     static constexpr int PLACES = 256;      // sub-blocks whose places are known at a time
     v8h k[2][2][4 * D], v[2][2][4 * D];     // [buffer][half of a piece][sub-block of the two steps][piece of 16 codes]
-    Place place[PLACES];
+    Spot place[PLACES];
     JoinShared join;
 };
 
@@ -618,23 +632,24 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const Item &it,
     State<D> s;
     clear(s);
 
-    const int heads = a.c.kv_heads, subs = a.c.page / SUB;
+    const int heads = a.c.kv_heads;
     const int kh = (col >> 2) & 1, ktok = 4 * (col >> 3) + (col & 3);
     const uint4 *kbase = static_cast<const uint4 *>(a.c.k), *vbase = static_cast<const uint4 *>(a.c.v);
     constexpr int PER = div_up(4 * D, THREADS);     // pieces of 16 bytes of a thread: two steps hold 4 D of each kind
     for (int batch = it.kt0; batch < it.kt1; batch += ManyShared<D>::PLACES / 2) {
         const int last = min(it.kt1, batch + ManyShared<D>::PLACES / 2), places = 2 * (last - batch);
         __syncthreads();
-        for (int i = tid; i < places; i += THREADS) sh.place[i] = place_of(a, it, head, 2 * batch + i, end);
+        for (int i = tid; i < places; i += THREADS) sh.place[i] = spot_of(a, it, head, 2 * batch + i, end);
         __syncthreads();
         uint4 rk[PER], rv[PER];
-        int id[PER];
+        bool gone[PER];
         auto fetch = [&](int kt) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
                 const int piece = tid + i * THREADS, sb = piece / D, in = piece - sb * D;
-                id[i] = sh.place[min(2 * (kt - batch) + sb, places - 1)].id;
-                const int64_t at = (((int64_t)max(id[i], 0) * heads + head) * subs + ((2 * kt + sb) & (subs - 1))) * D + in;
+                const Spot sp = sh.place[min(2 * (kt - batch) + sb, places - 1)];
+                gone[i] = sp.ks == 0.f;
+                const uint64_t at = (uint64_t)sp.at * D + in;
                 rk[i] = kbase[at];
                 rv[i] = vbase[at];
             }
@@ -644,9 +659,9 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const Item &it,
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
                 const int piece = tid + i * THREADS;
-                if (!whole || id[i] < 0) {          // bytes that may be anything: before the window, behind the last token, of no page
+                if (!whole || gone[i]) {            // bytes that may be anything: before the window, behind the last token, of no page
                     const int tok0 = kt * KT + piece / D * SUB;
-                    rv[i] = keep_bytes(rv[i], tile_lo - tok0, id[i] < 0 ? 0 : part_hi - tok0);
+                    rv[i] = keep_bytes(rv[i], tile_lo - tok0, gone[i] ? 0 : part_hi - tok0);
                 }
                 sh.k[buf][0][piece] = codes_to_half<FMT>(rk[i].x, rk[i].y);
                 sh.k[buf][1][piece] = codes_to_half<FMT>(rk[i].z, rk[i].w);
@@ -663,24 +678,21 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const Item &it,
             fetch(more ? kt + 2 : kt);              // no branch around a load
             const int tok = kt * KT;
             if (tok < any_hi && tok + 2 * KT > any_lo) {
-                Place pl[2];
                 float sc[2], lv[2], iv[2];
                 int tok0[2];
+                bool none = false;
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    pl[u] = sh.place[min(2 * (kt + u - batch) + h, places - 1)];
-                    sc[u] = factor * pl[u].ks;
-                    lv[u] = __builtin_amdgcn_logf(pl[u].vs);
-                    iv[u] = __builtin_amdgcn_rcpf(pl[u].vs);
-                    tok0[u] = tok + u * KT + SUB * h;
+                    const Spot sp = sh.place[min(2 * (kt + u - batch) + h, places - 1)];
+                    const bool dead = sp.ks == 0.f;
+                    sc[u] = dead ? 1.f : factor * sp.ks;
+                    lv[u] = sp.lv;
+                    iv[u] = sp.iv;
+                    tok0[u] = dead ? 0x40000000 : tok + u * KT + SUB * h;       // nowhere: as if behind all that the row sees
+                    none |= dead;
                 }
-                const bool edge = tok < all_lo || tok + 2 * KT > all_hi || __any(pl[0].id < 0 || pl[1].id < 0);
-                Sees mask{see.lo, min(see.hi, part_hi)};
-                // a sub-block that is nowhere: its tokens as if behind all that the row sees
-                if (edge) {
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) tok0[u] = pl[u].id < 0 ? 0x40000000 : tok0[u];
-                }
+                const bool edge = tok < all_lo || tok + 2 * KT > all_hi || __any(none);
+                const Sees mask{see.lo, min(see.hi, part_hi)};
                 steps<D, 2>(s, q, [&](int u, int i, int c) { return sh.k[buf][c][(2 * u + kh) * D + (2 * i + h) * 16 + ktok]; },
                             [&](int u, int n, int c) { return sh.v[buf][c][(2 * u + h) * D + n * 32 + col]; }, sc, lv, iv, edge, tok0, mask);
             }
