@@ -345,6 +345,19 @@ __device__ __forceinline__ void put2(float *p, float x, float y)
     __hip_atomic_store(reinterpret_cast<uint64_t *>(p), w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
+// Four numbers, through a descriptor of all parts' outputs.  16: of agent scope.
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ void put4(__amdgpu_buffer_rsrc_t rs, uint32_t at, float x, float y, float z, float w)
+{
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, make_float4(x, y, z, w)), rs, (int)(at * 4), 0, 16);
+}
+
+__device__ __forceinline__ float4 get4(__amdgpu_buffer_rsrc_t rs, uint32_t at)
+{
+    return __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(at * 4), 0, 16));
+}
+
 // (the address of all lanes, a lane's own bytes from there)
 __device__ __forceinline__ float get1(const float *p, uint32_t at)
 {
@@ -374,6 +387,35 @@ __device__ __forceinline__ bool all_parts_done(int32_t *count, int parts, JoinSh
     }
     __syncthreads();
     return sh.last;
+}
+
+// Maximum and sum of each row, into LDS; 1 to 64 lanes a row.
+__device__ __forceinline__ void join_sums(const AttendArgs &a, const Item &it, int head, const float *ml, int tile_rows, int threads, JoinShared &sh)
+{
+    const int tid = threadIdx.x, heads = a.c.kv_heads, rows = min(tile_rows, it.n_new * a.group - it.tile * tile_rows);
+    int pow2 = 4;
+    while (pow2 < rows) pow2 *= 2;
+    const int lanes = min(64, max(1, threads / pow2)), r = min(tid / lanes, rows - 1);
+    float top = -INFINITY, l = 0.f;
+    for (int p = tid % lanes; p < it.parts; p += lanes) {
+        const float2 v = get2(ml, (((it.part0 + p) * heads + head) * tile_rows + r) * 8u);
+        const float n = fmaxf(top, v.x);
+        l = n > -INFINITY ? l * exp2f(top - n) + v.y * exp2f(v.x - n) : l + v.y;      // the latter 0, or NaN
+        top = n;
+    }
+    for (int d = lanes / 2; d > 0; d >>= 1) {
+        const float m2 = __shfl_xor(top, d), l2 = __shfl_xor(l, d), n = fmaxf(top, m2);
+        l = n > -INFINITY ? l * exp2f(top - n) + l2 * exp2f(m2 - n) : l + l2;
+        top = n;
+    }
+    if (tid % lanes == 0 && tid / lanes < rows) {
+        sh.m[r] = top == -INFINITY ? 0.f : top;
+        sh.l[r] = l;
+        if (a.q.lse) {
+            const int row = it.tile * tile_rows + r, tok = row / a.group;
+            a.q.lse[(int64_t)(it.row0 + tok) * heads * a.group + head * a.group + row - tok * a.group] = l == 0.f ? -INFINITY : LN2 * (top + log2f(l));
+        }
+    }
 }
 
 // o: outputs [part][kv head][tile_rows][D], ml: [part][kv head][tile_rows][2]
@@ -406,29 +448,7 @@ __device__ __forceinline__ void join_parts(const AttendArgs &a, const Item &it, 
         }
     };
     fetch(e_first, g);
-    {   // maximum and sum of each row: 1 to 64 lanes a row
-        const int lanes = min(64, max(1, THREADS / pow2)), r = min(tid / lanes, rows - 1);
-        float top = -INFINITY, l = 0.f;
-        for (int p = tid % lanes; p < it.parts; p += lanes) {
-            const float2 v = get2(ml, at(p, r) * 8);
-            const float n = fmaxf(top, v.x);
-            l = n > -INFINITY ? l * exp2f(top - n) + v.y * exp2f(v.x - n) : l + v.y;      // the latter 0, or NaN
-            top = n;
-        }
-        for (int d = lanes / 2; d > 0; d >>= 1) {
-            const float m2 = __shfl_xor(top, d), l2 = __shfl_xor(l, d), n = fmaxf(top, m2);
-            l = n > -INFINITY ? l * exp2f(top - n) + l2 * exp2f(m2 - n) : l + l2;
-            top = n;
-        }
-        if (tid % lanes == 0 && tid / lanes < rows) {
-            sh.m[r] = top == -INFINITY ? 0.f : top;
-            sh.l[r] = l;
-            if (a.q.lse) {
-                const int row = it.tile * tile_rows + r, tok = row / a.group;
-                a.q.lse[(int64_t)(it.row0 + tok) * heads * a.group + head * a.group + row - tok * a.group] = l == 0.f ? -INFINITY : LN2 * (top + log2f(l));
-            }
-        }
-    }
+    join_sums(a, it, head, ml, tile_rows, THREADS, sh);
     __syncthreads();
     for (int e0 = 0; e0 < rows * QUADS; e0 += THREADS) {
         const int e = e0 + e_first, r = min(e / QUADS, rows - 1), d = (e % QUADS) * 4;
@@ -463,6 +483,68 @@ __device__ __forceinline__ void join_parts(const AttendArgs &a, const Item &it, 
             store4<DTYPE>(a.q.out, (it.row0 + tok) * a.q.out_stride + (int64_t)(head * a.group + row - tok * a.group) * D + d, a.vec_out, sum.x * f, sum.y * f, sum.z * f, sum.w * f);
         }
     }
+}
+
+// The same for tiles of 32 rows a wave: [part][kv head][wave][D / 8][64 lanes][4 dims], as the waves hold them (lane (h, row) has dims
+// 8 i + 4 h + (0..3)).  By rows, as above, a wave's store went to 64 places, eight bytes each: 128 tokens onto 8000 took 94 us,
+// 68 this way.  One block joins it all, so what counts is how many loads are on their way at once: those of SPAN parts of
+// each of ROUNDS rounds over the tile.
+template <int DTYPE, int D, int ROWS, int SPAN>
+__device__ __forceinline__ void join_tile_spans(const AttendArgs &a, const Item &it, int head, __amdgpu_buffer_rsrc_t o, const float *ml, JoinShared &sh)
+{
+    constexpr int THREADS = 64 * attend_waves(D), WAVE = 8 * D, AHEAD = 16, ROUNDS = AHEAD / SPAN;
+    const int tid = threadIdx.x, heads = a.c.kv_heads;
+    const int rows = min(ROWS, it.n_new * a.group - it.tile * ROWS), quads = div_up(rows, 32) * WAVE;
+    auto row_of = [&](int e) { return e / WAVE * 32 + e % 32; };
+    float m[AHEAD];
+    float4 x[AHEAD];
+    auto fetch = [&](int e0, int p0) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            if (p0 + u % SPAN >= it.parts) continue;
+            const int e = min(e0 + u / SPAN * THREADS, quads - 1);
+            const uint32_t at = (uint32_t)(((it.part0 + p0 + u % SPAN) * heads + head) * ROWS);
+            m[u] = get1(ml, (at + min(row_of(e), rows - 1)) * 8);
+            x[u] = get4(o, at * D + e * 4);
+        }
+    };
+    fetch(tid, 0);
+    join_sums(a, it, head, ml, ROWS, THREADS, sh);
+    __syncthreads();
+    for (int e0 = tid; e0 < quads; e0 += THREADS * ROUNDS) {
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int p0 = 0; p0 < it.parts; p0 += SPAN) {
+            if (e0 != tid || p0) fetch(e0, p0);
+#pragma unroll
+            for (int v = 0; v < ROUNDS; ++v) {
+                const int e = e0 + v * THREADS, r = min(row_of(e), rows - 1), d = e / 64 % (D / 8) * 8 + (e >> 5 & 1) * 4;
+                const float top = sh.m[r];
+#pragma unroll
+                for (int u = v * SPAN; u < (v + 1) * SPAN; ++u) {
+                    if (p0 + u % SPAN >= it.parts) continue;
+                    const float w = exp2f(m[u] - top);
+                    sum.x = fmaf(w, x[u].x, sum.x);
+                    sum.y = fmaf(w, x[u].y, sum.y);
+                    sum.z = fmaf(w, x[u].z, sum.z);
+                    sum.w = fmaf(w, x[u].w, sum.w);
+                }
+                if (p0 + SPAN < it.parts) continue;
+                if (row_of(e) < rows) {
+                    const float l = sh.l[r], f = l == 0.f ? 0.f : 1.f / l;
+                    const int row = it.tile * ROWS + r, tok = row / a.group;
+                    store4<DTYPE>(a.q.out, (it.row0 + tok) * a.q.out_stride + (int64_t)(head * a.group + row - tok * a.group) * D + d, a.vec_out, sum.x * f, sum.y * f, sum.z * f, sum.w * f);
+                }
+                sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+        }
+    }
+}
+
+template <int DTYPE, int D, int ROWS>
+__device__ __forceinline__ void join_tile(const AttendArgs &a, const Item &it, int head, __amdgpu_buffer_rsrc_t o, const float *ml, JoinShared &sh)
+{
+    if (it.parts <= 4) join_tile_spans<DTYPE, D, ROWS, 4>(a, it, head, o, ml, sh);
+    else join_tile_spans<DTYPE, D, ROWS, 16>(a, it, head, o, ml, sh);
 }
 
 // ---- a tile of 32 rows: every wave takes every eighth step of the block's, straight from memory into registers
@@ -704,9 +786,11 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const Item &it,
     s.l += __shfl_xor(s.l, 32);
     const bool whole = it.part < 0;
     float *ml = a.part_many + (int64_t)a.p.parts_many * heads * ROWS * D;
+    const __amdgpu_buffer_rsrc_t parts = __builtin_amdgcn_make_buffer_rsrc(a.part_many, 0, (int)((uint32_t)(a.p.parts_many * heads * ROWS) * (D * 4u)), 0x00020000);
     if (row.real) {
         const int tok = row.tok, g = row.g;
         const int64_t part = ((int64_t)it.part * heads + head) * ROWS + wave * 32 + col;
+        const uint32_t lane_at = (uint32_t)((it.part * heads + head) * ROWS + wave * 32) * D + lane * 4;
         const float f = whole ? (s.l == 0.f ? 0.f : 1.f / s.l) : 1.f;
         const int64_t out = (it.row0 + tok) * a.q.out_stride + (int64_t)(head * a.group + g) * D;
 #pragma unroll
@@ -718,8 +802,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const Item &it,
                 if (whole) {
                     store4<DTYPE>(a.q.out, out + d, a.vec_out, x, y, z, w);
                 } else {
-                    put2(a.part_many + part * D + d, x, y);
-                    put2(a.part_many + part * D + d + 2, z, w);
+                    put4(parts, lane_at + (4 * n + i) * 256, x, y, z, w);
                 }
             }
         if (h == 0) {
@@ -727,7 +810,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const Item &it,
             else if (a.q.lse) a.q.lse[(int64_t)(it.row0 + tok) * heads * a.group + head * a.group + g] = s.l == 0.f ? -INFINITY : LN2 * (s.m + log2f(s.l));
         }
     }
-    if (!whole && all_parts_done(a.p.joins_many + it.join * heads + head, it.parts, sh.join)) join_parts<DTYPE, D>(a, it, head, a.part_many, ml, ROWS, sh.join);
+    if (!whole && all_parts_done(a.p.joins_many + it.join * heads + head, it.parts, sh.join)) join_tile<DTYPE, D, ROWS>(a, it, head, parts, ml, sh.join);
 }
 
 template <int DTYPE, int FMT, int D>
