@@ -422,7 +422,7 @@ __device__ __forceinline__ void join_sums(const AttendArgs &a, const Item &it, i
 template <int DTYPE, int D>
 __device__ __forceinline__ void join_parts(const AttendArgs &a, const Item &it, int head, const float *o, const float *ml, int tile_rows, JoinShared &sh)
 {
-    constexpr int THREADS = 64 * attend_waves(D);
+    constexpr int THREADS = 64 * ATTEND_WAVES;
     const int tid = threadIdx.x, heads = a.c.kv_heads;
     const int rows = min(tile_rows, it.n_new * a.group - it.tile * tile_rows);
     int pow2 = 4;
@@ -492,7 +492,7 @@ __device__ __forceinline__ void join_parts(const AttendArgs &a, const Item &it, 
 template <int DTYPE, int D, int ROWS, int SPAN>
 __device__ __forceinline__ void join_tile_spans(const AttendArgs &a, const Item &it, int head, __amdgpu_buffer_rsrc_t o, const float *ml, JoinShared &sh)
 {
-    constexpr int THREADS = 64 * attend_waves(D), WAVE = 8 * D, AHEAD = 16, ROUNDS = AHEAD / SPAN;
+    constexpr int THREADS = 64 * ATTEND_WAVES, WAVE = 8 * D, AHEAD = 16, ROUNDS = AHEAD / SPAN;
     const int tid = threadIdx.x, heads = a.c.kv_heads;
     const int rows = min(ROWS, it.n_new * a.group - it.tile * ROWS), quads = div_up(rows, 32) * WAVE;
     auto row_of = [&](int e) { return e / WAVE * 32 + e % 32; };
@@ -550,15 +550,15 @@ __device__ __forceinline__ void join_tile(const AttendArgs &a, const Item &it, i
 // ---- a tile of 32 rows: every wave takes every eighth step of the block's, straight from memory into registers
 template <int D>
 struct FewShared {
-    float m[attend_waves(D)][ROWS_FEW], l[attend_waves(D)][ROWS_FEW];
-    __align__(16) float o[attend_waves(D) * 8 * (D + 4)];
+    float m[ATTEND_WAVES][ROWS_FEW], l[ATTEND_WAVES][ROWS_FEW];
+    __align__(16) float o[ATTEND_WAVES * 8 * (D + 4)];
     JoinShared join;
 };
 
 template <int DTYPE, int FMT, int D>
 __device__ __forceinline__ void attend_few(const AttendArgs &a, const Item &it, int head, FewShared<D> &sh)
 {
-    constexpr int WAVES = attend_waves(D);
+    constexpr int WAVES = ATTEND_WAVES;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 31, h = lane >> 5;
     const int rows = it.n_new * a.group, row0 = it.tile * ROWS_FEW, here = min(ROWS_FEW, rows - row0);
     const Row row = row_at(a, row0, row0 + col, rows);
@@ -696,7 +696,7 @@ struct ManyShared {
 template <int DTYPE, int FMT, int D>
 __device__ __forceinline__ void attend_many(const AttendArgs &a, const Item &it, int head, ManyShared<D> &sh)
 {
-    constexpr int THREADS = 64 * attend_waves(D), ROWS = 32 * attend_waves(D);
+    constexpr int THREADS = 64 * ATTEND_WAVES, ROWS = 32 * ATTEND_WAVES;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 31, h = lane >> 5;
     const int rows = it.n_new * a.group, tile0 = it.tile * ROWS, row0 = tile0 + wave * 32;
     const Row row = row_at(a, tile0, row0 + col, rows);
@@ -814,7 +814,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const Item &it,
 }
 
 template <int DTYPE, int FMT, int D>
-__global__ void __launch_bounds__(64 * attend_waves(D), D <= 128 ? 2 : 1) k_kv_attend(AttendArgs a)
+__global__ void __launch_bounds__(64 * ATTEND_WAVES, D <= 128 ? 2 : 1) k_kv_attend(AttendArgs a)
 {
     __shared__ union {
         FewShared<D> few;

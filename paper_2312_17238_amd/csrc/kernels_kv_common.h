@@ -14,17 +14,25 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 
 constexpr int SUB = 16;            // tokens of a 16 x 16 tile of codes
 constexpr int KT = 32;             // tokens of a step of the attention kernels: the rows of one matrix instruction
-// Waves of a block of the attention: two on every SIMD of a compute unit; heads of 256 take the registers of both for one.
-__host__ __device__ constexpr int attend_waves(int head_dim) { return head_dim <= 128 ? 4 : 4; }
+constexpr int ATTEND_WAVES = 4;    // of a block of the attention, two blocks a compute unit; heads of 256 take the registers of both for one
 constexpr int ROWS_FEW = 32;       // (token, query head of the group) rows of a block whose waves share out the cached tokens
-constexpr int FEW_MOST = 64;       // requests of up to this many rows are made of such blocks; the others of blocks whose waves
-                                   // share out the rows, 32 to each
+// Requests of up to this many rows are made of such blocks; the others of blocks whose waves share out the rows, 32 to each.  At
+// 32, 64 and 128: 40 rows of 24 requests 17.1, 13.4 and 13.4 us; 96 rows of 16 requests 60.8, 60.8 and 40.7, but the pages of 2048
+// requests 12.6, 12.6 and 17.1, as the plan then holds four tiles of a request in registers.
+constexpr int FEW_MOST = 64;
 constexpr int COMPUTE_UNITS = 256;
-constexpr int BLOCKS_FEW = 2 * COMPUTE_UNITS;    // blocks that the cached tokens of small requests are shared out to: two a compute unit
-constexpr int BLOCKS_MANY = 512;
-constexpr int MIN_KT_FEW = 16;     // steps of a block at least
-constexpr int SPLIT_STEPS = 32;    // what joining a tile's parts costs, in steps of a block
-constexpr int MIN_KT_MANY = 16;
+// Blocks that cached tokens are shared out to.  With 256 for the many, 512 tokens onto 6000 take 102.6 us instead of 99, with 1024 a
+// prompt of 4096 takes 200 instead of 165 (its tiles are split then); for the few, the decode kernel says.
+constexpr int BLOCKS_FEW = 2 * COMPUTE_UNITS;
+constexpr int BLOCKS_MANY = 2 * COMPUTE_UNITS;
+// Steps of a block at least.  Few: one token onto 4000 takes 13.0, 10.5 and 15.4 us at 4, 16 and 64, 11.1 at 24; 8 requests of a token onto
+// 2000 to 2600 14.6 at 16, 13.5 at 24, 8 of 4 tokens onto 3000 18.8 and 16.9.  Many: 128 tokens onto 8000 take 68.5 us at 16, 52.7 at 32; 2
+// requests of 24 tokens onto 3000 32.4 and 36.2.
+constexpr int MIN_KT_FEW = 24, MIN_KT_MANY = 32;
+// What joining a tile's parts costs, in steps of a block, and what a block's second tile costs besides.  SPLIT_STEPS at 8, 32 and 128: 24 requests
+// of 40 rows that see 1024 tokens 24.9, 13.4 and 13.4 us, one of a token onto 4000 10.7, 10.5 and 18.6.  LINE_STEPS at 0, 64
+// and 128: 8 requests of a token onto 2000 to 2600 20.5, 14.6 and 14.8, 64 of a token onto 500 to 8000 67.7, 68.0 and 75.0.
+constexpr int SPLIT_STEPS = 32, LINE_STEPS = 64;
 
 // A piece of work, for each kv head: rows [tile * ROWS, ...) of a request against the cached tokens [kt0, kt1) * KT.
 struct __align__(16) Item {

@@ -118,6 +118,26 @@ __host__ __device__ __forceinline__ int share(double all, int target, int least)
     return even > least ? even : least;
 }
 
+// Tiles of few rows: the steps of a block.
+__host__ __device__ __forceinline__ uint32_t first_chunk(uint32_t line, uint32_t tiles, uint32_t target)
+{
+    const uint32_t even = (line + target - 1) / target, least = tiles <= target ? MIN_KT_FEW : 1;
+    return even > least ? even : least;
+}
+
+// Where there is a block for every tile (tiles <= target): the steps of a block if tiles begin with a block of their own, 0 if they had better
+// not.  `blocks`: how many blocks first_chunk's steps would make that way, where the longest tile takes more than one.
+// Costs are compared in steps: SPLIT_STEPS to join a tile's parts, LINE_STEPS for a block with the end of one tile and the beginning of another.
+__host__ __device__ __forceinline__ uint32_t own_chunk(uint32_t line, uint32_t tiles, uint32_t target, uint32_t longest, uint32_t chunk, uint32_t blocks)
+{
+    if (longest <= chunk + SPLIT_STEPS) return longest > 1 ? longest : 1;      // a tile a block
+    if (blocks <= target) return chunk;
+    // of c steps there are no more than (line + tiles (c - 1)) / c blocks
+    uint32_t own = tiles < target ? (line - tiles + target - tiles - 1) / (target - tiles) : longest;
+    if (longest <= own + SPLIT_STEPS) own = longest;
+    return own + (own < longest ? SPLIT_STEPS : 0) <= chunk + SPLIT_STEPS + LINE_STEPS ? own : 0;
+}
+
 // Writes the items of one tile, in as many parts as `n`.
 __device__ __forceinline__ void put_items(Item *items, Item it, int n, int item0, int join, int part0)
 {
@@ -214,11 +234,10 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
     if (role == 0) {
         // what is per request, and the requests of few rows
         block_scan<THREADS>(used, tmp, &total);
-        // Tiles of 32 rows, one after the other on a line of steps (a tile that sees nothing takes one step of it): every
-        // block gets a piece of the line of the same length, whatever tiles begin and end in it.  A tile that lies in several
-        // pieces is joined from its parts.  Where there is a block for every tile and the longest tile is not much longer than such a piece
-        // each block gets a tile instead: to join parts costs what SPLIT_STEPS steps cost.
-        // Sums stay below 2^32: 8192 tiles of less than 2^19 steps.
+        // Tiles of 32 rows, one after the other on a line of steps (a tile that sees nothing takes one step of it), cut into blocks of
+        // `chunk` steps.  Either every block gets a piece of the line of the same length, whatever tiles begin and end in it; or
+        // each tile begins with a block of its own (its end is padded to a whole chunk), where there are blocks enough for that: see share_tiles.
+        // Sums stay below 2^32: 8192 tiles of less than 2^19 steps, or 768 blocks of as many.
         constexpr int TILES = FEW_MOST / ROWS_FEW;
         int tiles[PER], kt0[PER][TILES], kt1[PER][TILES];
         uint32_t steps = 0, line, longest = 0, n_tiles = 0, all_tiles;
@@ -247,28 +266,35 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
             a.io.free_left[0] = free_n - (int)total;
         }
         const uint32_t start = block_scan<THREADS>(steps, tmp, &line) - steps;
-        const uint32_t tile0 = block_scan<THREADS>(n_tiles, tmp, &all_tiles) - n_tiles;
-        const uint32_t even = (line + a.target_few - 1) / a.target_few;
-        const uint32_t chunk = all_tiles <= (uint32_t)a.target_few ? max((uint32_t)MIN_KT_FEW, even) : max(1u, even);
-        const bool whole = block_max<THREADS>(longest, tmp) <= chunk + SPLIT_STEPS && all_tiles <= (uint32_t)a.target_few;
-        if (whole) {
-            uint32_t at = tile0;
+        block_scan<THREADS>(n_tiles, tmp, &all_tiles);
+        longest = block_max<THREADS>(longest, tmp);
+        const uint32_t target = (uint32_t)a.target_few;
+        bool apart = false;
+        uint32_t chunk = first_chunk(line, all_tiles, target), pos = start;
+        if (all_tiles <= target) {
+            uint32_t at = 0, all = 0;
+            auto blocks_of_chunk = [&] {
+                uint32_t n = 0;
 #pragma unroll
-            for (int i = 0; i < PER; ++i)
+                for (int i = 0; i < PER; ++i)
 #pragma unroll
-                for (int t = TILES - 1; t >= 0; --t)
-                    if (t < tiles[i]) {
-                        a.p.few[at] = Item{r0 + i, first[i], now[i], ctx[i], t, kt0[i][t], kt1[i][t], -1, 0, 1, 0, 0};
-                        a.p.few_first[at] = (int)at;
-                        ++at;
-                    }
-            if (tid == 0) {
-                a.p.head->few_blocks = (int)all_tiles;
-                a.p.few_first[all_tiles] = (int)all_tiles;
+                    for (int t = 0; t < TILES; ++t)
+                        if (t < tiles[i]) n += (max(1, kt1[i][t] - kt0[i][t]) + chunk - 1) / chunk;
+                at = block_scan<THREADS>(n, tmp, &all) - n;
+            };
+            if (longest > chunk + SPLIT_STEPS) blocks_of_chunk();
+            const uint32_t own = own_chunk(line, all_tiles, target, longest, chunk, all);
+            if (own) {
+                apart = true;
+                chunk = own;
+                blocks_of_chunk();
+                pos = at * chunk;
+                line = all * chunk;
             }
-            return;
         }
-        uint32_t items = 0, split = 0, pos = start;      // split: joins << 16 | parts
+        const uint32_t begin = pos;
+        uint32_t items = 0, split = 0;      // split: joins << 16 | parts
+        auto next_at = [&](uint32_t end) { return apart ? (end + chunk - 1) / chunk * chunk : end; };
         uint32_t b0[PER][TILES], parts[PER][TILES];
 #pragma unroll
         for (int i = 0; i < PER; ++i)
@@ -280,11 +306,11 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
                     const uint32_t n = parts[i][t] = (pos + len - 1) / chunk - b0[i][t] + 1;
                     items += n;
                     split += n > 1 ? (1u << 16) + n : 0;
-                    pos += len;
+                    pos = next_at(pos + len);
                 }
         uint32_t all_items, all_split;
         uint32_t item0 = block_scan<THREADS>(items, tmp, &all_items) - items, split0 = block_scan<THREADS>(split, tmp, &all_split) - split;
-        pos = start;
+        pos = begin;
 #pragma unroll
         for (int i = 0; i < PER; ++i)
 #pragma unroll
@@ -303,7 +329,7 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
                     }
                     item0 += n;
                     split0 += n > 1 ? (1u << 16) + n : 0;
-                    pos += max(1, len);
+                    pos = next_at(pos + max(1, len));
                 }
         if (tid == 0) {
             const uint32_t blocks = (line + chunk - 1) / chunk;

@@ -83,7 +83,7 @@ static int target_blocks(int blocks, int heads) { return std::max(1, blocks / he
 static Sizes sizes_of(const moe_kv_step_t *s)
 {
     Sizes z{};
-    z.rows_many = 32 * attend_waves(s->head_dim);
+    z.rows_many = 32 * ATTEND_WAVES;
     z.group = s->q_heads / s->kv_heads;
     z.new_most = std::min(s->max_new, s->n_tokens);
     z.many = (int64_t)z.new_most * z.group > FEW_MOST;
@@ -263,9 +263,9 @@ static void launch_attend(const AttendArgs &a, int D, bool decode, dim3 grid, hi
         return;
     }
     switch (D) {
-    case 64: hipLaunchKernelGGL((k_kv_attend<DTYPE, FMT, 64>), grid, dim3(64 * attend_waves(64)), 0, s, a); break;
-    case 128: hipLaunchKernelGGL((k_kv_attend<DTYPE, FMT, 128>), grid, dim3(64 * attend_waves(128)), 0, s, a); break;
-    default: hipLaunchKernelGGL((k_kv_attend<DTYPE, FMT, 256>), grid, dim3(64 * attend_waves(256)), 0, s, a); break;
+    case 64: hipLaunchKernelGGL((k_kv_attend<DTYPE, FMT, 64>), grid, dim3(64 * ATTEND_WAVES), 0, s, a); break;
+    case 128: hipLaunchKernelGGL((k_kv_attend<DTYPE, FMT, 128>), grid, dim3(64 * ATTEND_WAVES), 0, s, a); break;
+    default: hipLaunchKernelGGL((k_kv_attend<DTYPE, FMT, 256>), grid, dim3(64 * ATTEND_WAVES), 0, s, a); break;
     }
 }
 

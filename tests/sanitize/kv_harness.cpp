@@ -90,20 +90,24 @@ int main()
                 }
                 need(items <= p.max_many && parts <= p.parts_many && joins <= p.max_joins_many, "lists of many rows", run);
             } else {
-                const long long target = p.blocks_few, even = (line + target - 1) / target, tiles = (long long)len.size();
-                const long long chunk = tiles <= target ? std::max<long long>(MIN_KT_FEW, even) : std::max<long long>(1, even);
-                if (longest <= chunk + SPLIT_STEPS && tiles <= target) {
-                    items = tiles;
-                } else {
-                    long long pos = 0;
-                    for (int l : len) {
-                        const long long w = std::max(1, l), n = (pos + w - 1) / chunk - pos / chunk + 1;
-                        items += n;
-                        if (n > 1) { parts += n; ++joins; }
-                        pos += w;
-                    }
-                    need((line + chunk - 1) / chunk <= p.blocks_few, "blocks", run);
+                const long long target = p.blocks_few, tiles = (long long)len.size();
+                uint32_t chunk = first_chunk((uint32_t)line, (uint32_t)tiles, (uint32_t)target), own = 0;
+                if (tiles <= target) {
+                    long long blocks = 0;
+                    for (int l : len) blocks += (std::max(1, l) + chunk - 1) / chunk;
+                    own = own_chunk((uint32_t)line, (uint32_t)tiles, (uint32_t)target, (uint32_t)longest, chunk, (uint32_t)blocks);
+                    if (own) chunk = own;
                 }
+                long long pos = 0;
+                for (int l : len) {
+                    const long long w = std::max(1, l), n = (pos + w - 1) / chunk - pos / chunk + 1;
+                    items += n;
+                    if (n > 1) { parts += n; ++joins; }
+                    pos += w;
+                    if (own) pos = (pos + chunk - 1) / chunk * chunk;
+                    need(pos < (1ll << 32), "32-bit line", run);
+                }
+                need((pos + chunk - 1) / chunk <= p.blocks_few, "blocks", run);
                 need(items <= p.max_few && parts <= p.parts_few && joins <= p.max_joins_few, "lists of few rows", run);
             }
             need(parts < 65536 && joins < 65536, "packed sums", run);
