@@ -44,7 +44,7 @@ enum {
 };
 
 typedef struct {
-    int32_t n_pages;
+    int32_t n_pages;          /* n_pages * page < 2^31 and n_pages * kv_heads * page / 16 < 2^32                 */
     int32_t page;             /* tokens per page: 16, 32, 64 or 128                                              */
     int32_t kv_heads;         /* 1..256                                                                          */
     int32_t head_dim;         /* 64, 128 or 256                                                                  */
@@ -59,7 +59,7 @@ typedef struct {
     int32_t n_requests;       /* 1..MOE_KV_MAX_REQUESTS                                                          */
     int32_t n_tokens;         /* rows of the batch, 1..MOE_KV_MAX_TOKENS; rows past the last request's are left alone */
     int32_t max_new;          /* no request brings more rows than this (those that do are BAD_SIZE)              */
-    int32_t max_blocks;       /* width of the block table                                                        */
+    int32_t max_blocks;       /* width of the block table; max_blocks * page < 2^24 tokens of a request          */
     int32_t n_pages, page, kv_heads, head_dim;   /* as the caches that the step runs on                          */
     int32_t q_heads;          /* a multiple of kv_heads; query head h reads kv head h / (q_heads / kv_heads)     */
     int32_t causal;           /* 1: a token sees the tokens up to itself; 0: all of its request                  */
@@ -92,7 +92,8 @@ uint64_t moe_kv_scratch_bytes(const moe_kv_step_t *step);
  * it and the requests before it need (those that were turned down for want of pages included) are not more than the free
  * ones; they are taken off the stack's top, in order.  A request with a status gets nothing: its rows have no slot and attend
  * to nothing (those of a BAD_SIZE request are left alone).  A slot is -1, too, where the table or the stack names a page that does not exist.
- * plan_dev: moe_kv_plan_bytes, 256-byte aligned: what moe_kv_write and moe_kv_attend read. */
+ * plan_dev: moe_kv_plan_bytes, 256-byte aligned: what moe_kv_write and moe_kv_attend read, with the step that it was made for.  One
+ * moe_kv_attend at a time uses a plan (it counts the parts that are done there). */
 int32_t moe_kv_plan(const moe_kv_step_t *step, const moe_kv_lists_t *lists, void *plan_dev, void *stream);
 
 /* Give back all pages of `n` requests (ids in `requests`, dev; out of range or repeated ones do nothing more), in the order given: their

@@ -158,7 +158,9 @@ __device__ __forceinline__ void put_items(Item *items, Item it, int n, int item0
     }
 }
 
-// THREADS: a thread has at most PER requests.  64 threads, whose sums need no LDS and no barrier, are MEASURED_PLAN.
+// THREADS: a thread has at most PER requests.  One wave's sums need no LDS and no barrier: 8 requests take 3.5 us with 64 threads and 5.0 with
+// 256, 200 requests 5.1 with 256 and 6.9 with 1024.  2048 requests of 77 thousand rows take 12.6 us; with one block for the requests of
+// many rows 14.8, with that block sharing out the others' too 17.
 template <int THREADS, int PER>
 __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
 {
