@@ -59,7 +59,7 @@ typedef struct {
     int32_t n_requests;       /* 1..MOE_KV_MAX_REQUESTS                                                          */
     int32_t n_tokens;         /* rows of the batch, 1..MOE_KV_MAX_TOKENS; rows past the last request's are left alone */
     int32_t max_new;          /* no request brings more rows than this (those that do are BAD_SIZE)              */
-    int32_t max_blocks;       /* width of the block table; max_blocks * page < 2^24 tokens of a request          */
+    int32_t max_blocks;       /* width of the block table; max_blocks * page <= 2^24 - 32 tokens of a request    */
     int32_t n_pages, page, kv_heads, head_dim;   /* as the caches that the step runs on                          */
     int32_t q_heads;          /* a multiple of kv_heads; query head h reads kv head h / (q_heads / kv_heads)     */
     int32_t causal;           /* 1: a token sees the tokens up to itself; 0: all of its request                  */

@@ -111,11 +111,12 @@ __host__ __device__ __forceinline__ void key_steps(const moe_kv_step_t &s, int c
     kt1 = (hi + KT - 1) / KT;
 }
 
-// The steps of a block where `all` steps are shared out to `target` blocks of at least `least`.
+// The steps of a block where `all` steps are shared out to `target` blocks of at least `least`.  A million rows of a thousand heads
+// have up to 2^42 steps: no tile is split from 2^19 on, so what a block gets beyond an int is cut off.
 __host__ __device__ __forceinline__ int share(double all, int target, int least)
 {
-    const int even = (int)(((int64_t)all + target - 1) / target);
-    return even > least ? even : least;
+    const int64_t even = ((int64_t)all + target - 1) / target;
+    return even > least ? even < 0x7FFFFFFF ? (int)even : 0x7FFFFFFF : least;
 }
 
 // Tiles of few rows: the steps of a block.
@@ -239,7 +240,7 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
         // Tiles of 32 rows, one after the other on a line of steps (a tile that sees nothing takes one step of it), cut into blocks of
         // `chunk` steps.  Either every block gets a piece of the line of the same length, whatever tiles begin and end in it; or
         // each tile begins with a block of its own (its end is padded to a whole chunk), where there are blocks enough for that: see share_tiles.
-        // Sums stay below 2^32: 8192 tiles of less than 2^19 steps, or 768 blocks of as many.
+        // Sums, and what is added to them to round up, stay below 2^32: 8192 tiles of less than 2^19 steps, or 768 blocks of as many.
         constexpr int TILES = FEW_MOST / ROWS_FEW;
         int tiles[PER], kt0[PER][TILES], kt1[PER][TILES];
         uint32_t steps = 0, line, longest = 0, n_tiles = 0, all_tiles;

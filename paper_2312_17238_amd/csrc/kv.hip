@@ -46,7 +46,7 @@ static bool step_ok(const moe_kv_step_t *s)
 {
     return s && s->n_requests >= 1 && s->n_requests <= MOE_KV_MAX_REQUESTS && s->n_tokens >= 1 && s->n_tokens <= MOE_KV_MAX_TOKENS &&
            s->max_new >= 1 && s->max_blocks >= 1 && geometry_ok(s->n_pages, s->page, s->kv_heads, s->head_dim) &&
-           (int64_t)s->max_blocks * s->page < (1ll << 24) && s->q_heads >= 1 && s->q_heads <= 1024 && s->q_heads % s->kv_heads == 0 &&
+           (int64_t)s->max_blocks * s->page <= (1ll << 24) - KT && s->q_heads >= 1 && s->q_heads <= 1024 && s->q_heads % s->kv_heads == 0 &&
            (s->causal == 0 || s->causal == 1) && s->window >= 0 && s->reserved == 0;
 }
 
