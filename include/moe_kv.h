@@ -73,7 +73,8 @@ typedef struct {
     const int32_t *new_len;     /* [n_requests] tokens that this step adds                                       */
     int32_t *block_table;       /* [n_requests][max_blocks]: page of tokens [b page, (b+1) page).  Entries up to
                                    ceil(ctx_len/page) are read, those of the pages a step adds are written       */
-    const int32_t *free_pages;  /* a stack of at most n_pages free pages, its top at [*free_count - 1]           */
+    const int32_t *free_pages;  /* a stack of at most n_pages free pages, its top at [*free_count - 1]; the first min(*free_count,
+                                   n_pages) entries may be read (moe_kv_plan_within: no more than free_capacity)  */
     const int32_t *free_count;
     int32_t *row_start;         /* out [n_requests + 1]: first row of each request                               */
     int32_t *positions;         /* out [n_tokens]: position of a row's token in its request, -1 for none         */
@@ -95,6 +96,8 @@ uint64_t moe_kv_scratch_bytes(const moe_kv_step_t *step);
  * plan_dev: moe_kv_plan_bytes, 256-byte aligned: what moe_kv_write and moe_kv_attend read, with the step that it was made for.  One
  * moe_kv_attend at a time uses a plan (it counts the parts that are done there). */
 int32_t moe_kv_plan(const moe_kv_step_t *step, const moe_kv_lists_t *lists, void *plan_dev, void *stream);
+/* The same with a stack that has room for free_capacity entries: a *free_count above it counts as free_capacity. */
+int32_t moe_kv_plan_within(const moe_kv_step_t *step, const moe_kv_lists_t *lists, int32_t free_capacity, void *plan_dev, void *stream);
 
 /* Give back all pages of `n` requests (ids in `requests`, dev; out of range or repeated ones do nothing more), in the order given: their
  * pages go onto the stack, ctx_len[r] becomes 0.  Pages that are no page of the cache, and those that find the

@@ -33,7 +33,7 @@ MOE_KV_MAX_REQUESTS, MOE_KV_MAX_TOKENS = 4096, 1048576
 MOE_KV_E4M3, MOE_KV_INT8 = 0, 1
 MOE_KV_F16, MOE_KV_BF16 = 0, 1
 MOE_KV_SERVED, MOE_KV_NO_PAGES, MOE_KV_TOO_LONG, MOE_KV_BAD_SIZE = 0, 1, 2, 3
-KV_EXPORTS = ["moe_kv_plan_bytes", "moe_kv_scratch_bytes", "moe_kv_plan", "moe_kv_release", "moe_kv_write", "moe_kv_attend",
+KV_EXPORTS = ["moe_kv_plan_bytes", "moe_kv_scratch_bytes", "moe_kv_plan", "moe_kv_plan_within", "moe_kv_release", "moe_kv_write", "moe_kv_attend",
               "moe_kv_gather"]
 
 
@@ -192,6 +192,7 @@ def lib() -> C.CDLL:
     L.moe_kv_scratch_bytes.restype = u64
     L.moe_kv_scratch_bytes.argtypes = [C.POINTER(KvStep)]
     L.moe_kv_plan.argtypes = [C.POINTER(KvStep), C.POINTER(KvLists), vp, vp]
+    L.moe_kv_plan_within.argtypes = [C.POINTER(KvStep), C.POINTER(KvLists), i32, vp, vp]
     L.moe_kv_release.argtypes = [vp, i32, i32, i32, i32, i32, vp, vp, vp, i32, vp, vp]
     L.moe_kv_write.argtypes = [C.POINTER(KvCache), C.POINTER(KvStep), vp, C.POINTER(KvRows), vp]
     L.moe_kv_attend.argtypes = [C.POINTER(KvCache), C.POINTER(KvStep), vp, vp, C.POINTER(KvQuery), vp, u64, vp]
@@ -375,6 +376,10 @@ def moe_kv_scratch_bytes(step: KvStep) -> int:
 
 def moe_kv_plan(step: KvStep, lists: KvLists, plan_dev: int, stream: int) -> None:
     check(lib().moe_kv_plan(C.byref(step), C.byref(lists), plan_dev, stream))
+
+
+def moe_kv_plan_within(step: KvStep, lists: KvLists, free_capacity: int, plan_dev: int, stream: int) -> None:
+    check(lib().moe_kv_plan_within(C.byref(step), C.byref(lists), free_capacity, plan_dev, stream))
 
 
 def moe_kv_release(requests: int, n: int, n_requests: int, n_pages: int, page: int, max_blocks: int, ctx_len: int,

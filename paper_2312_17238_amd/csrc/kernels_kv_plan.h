@@ -19,6 +19,7 @@ struct PlanArgs {
     moe_kv_step_t s;
     moe_kv_lists_t io;
     Plan p;
+    int32_t free_most;      // entries of the stack that may be read
     int32_t group, page_shift, target_few, target_many, rows_many;
     int32_t many_blocks;    // blocks that share out the requests of many rows
 };
@@ -172,7 +173,7 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
     const int R = s.n_requests, T = s.n_tokens, tid = threadIdx.x, page = s.page, shift = a.page_shift;
     int32_t *row_end = lds, *need_before = lds + R, *sums = lds + 2 * R;   // sums: what the block's own role needs
     const int per = PER == 1 ? 1 : div_up(R, THREADS), r0 = tid * per;
-    const int free_n = min(max(0, a.io.free_count[0]), s.n_pages);
+    const int free_n = min(max(0, a.io.free_count[0]), a.free_most);
     auto pages = [&](int n) { return (int)(((uint32_t)n + page - 1) >> shift); };      // n < 2^31
 
     // rows

@@ -150,7 +150,13 @@ extern "C" uint64_t moe_kv_scratch_bytes(const moe_kv_step_t *step)
 
 extern "C" int32_t moe_kv_plan(const moe_kv_step_t *step, const moe_kv_lists_t *io, void *plan_dev, void *stream)
 {
+    return moe_kv_plan_within(step, io, step ? step->n_pages : 1, plan_dev, stream);
+}
+
+extern "C" int32_t moe_kv_plan_within(const moe_kv_step_t *step, const moe_kv_lists_t *io, int32_t free_capacity, void *plan_dev, void *stream)
+{
     if (!step_ok(step)) return bad("moe_kv_plan: bad or unsupported step");
+    if (free_capacity < 1) return bad("moe_kv_plan: a stack of %d free pages", free_capacity);
     if (!io || !plan_dev || ((uintptr_t)plan_dev & 255)) return bad("moe_kv_plan: null lists, or a plan that is null or not 256-byte aligned");
     const void *in[] = {io->ctx_len, io->new_len, io->free_pages, io->free_count, io->block_table};
     const void *out[] = {io->row_start, io->positions, io->slots, io->kv_len, io->status, io->free_left};
@@ -162,7 +168,7 @@ extern "C" int32_t moe_kv_plan(const moe_kv_step_t *step, const moe_kv_lists_t *
             if (p == q) return bad("moe_kv_plan: an output is an input");
     }
     const Sizes z = sizes_of(step);
-    PlanArgs a{*step, *io, plan_at(z, step->kv_heads, plan_dev), z.group, log2_of(step->page), z.p.blocks_few, target_blocks(BLOCKS_MANY, step->kv_heads), z.rows_many, std::min(8, std::max(1, div_up(z.p.max_many, PLAN_MOST_THREADS)))};
+    PlanArgs a{*step, *io, plan_at(z, step->kv_heads, plan_dev), std::min(free_capacity, step->n_pages), z.group, log2_of(step->page), z.p.blocks_few, target_blocks(BLOCKS_MANY, step->kv_heads), z.rows_many, std::min(8, std::max(1, div_up(z.p.max_many, PLAN_MOST_THREADS)))};
     const int R = step->n_requests, threads = R <= 64 ? 64 : R <= 256 ? 256 : PLAN_MOST_THREADS;
     const dim3 grid(1 + a.many_blocks + std::min(240, div_up(std::max(step->n_tokens, z.p.max_segments), threads)));
     const size_t lds = (size_t)R * 12;

@@ -106,13 +106,14 @@ class Step:
         self._scale = 1.0 / math.sqrt(head_dim)
 
     def plan(self, ctx_len, new_len, block_table, free_pages, free_count) -> None:
-        """Pages for the step's new tokens (block_table is updated in place, ctx_len and the stack stay until `advance`)."""
+        """Pages for the step's new tokens (block_table is updated in place, ctx_len and the stack stay until `advance`).
+        A free_count above the length of free_pages counts as that length."""
         x = self._lists
         x.ctx_len, x.new_len = _ints(ctx_len, self._per_request, "ctx_len"), _ints(new_len, self._per_request, "new_len")
         x.block_table = _ints(block_table, self._table, "block_table")
         _need(free_pages.dim() == 1 and free_pages.numel() >= 1, "plan: free_pages is a list")
         x.free_pages, x.free_count = _ints(free_pages, free_pages.shape, "free_pages"), _ints(free_count, (1,), "free_count")
-        rc = B.lib().moe_kv_plan(self._ref, self._lists_ref, self.plan_dev.data_ptr(), _stream(self.plan_dev))
+        rc = B.lib().moe_kv_plan_within(self._ref, self._lists_ref, free_pages.numel(), self.plan_dev.data_ptr(), _stream(self.plan_dev))
         if rc:
             B.check(rc)
         self.block_table, self._ctx, self._count = block_table, ctx_len, free_count
