@@ -7,7 +7,8 @@
     out = attend(cache, step, q)                                        # per layer
     step.advance()                                                      # the new tokens are cached ones now
 
-Everything runs on torch's current stream and reads no length on the host.  All lists of numbers are int32 tensors on the device.
+The step, the cache and all tensors of a call are on one GPU; everything runs on torch's current stream of that GPU (which need not be the
+current one) and reads no length on the host.  All lists of numbers are int32 tensors on the device.
 """
 from __future__ import annotations
 
@@ -26,8 +27,16 @@ FORMATS = {torch.float8_e4m3fn: B.MOE_KV_E4M3, torch.int8: B.MOE_KV_INT8}
 # messages only when something is refused.
 
 
-def _stream(t: torch.Tensor) -> int:
-    return torch._C._cuda_getCurrentRawStream(t.device.index)
+def _call(fn, device: int, *args) -> None:
+    """fn(*args, stream): on the device's current stream, with the device current, for a default stream is 0 on all of them."""
+    stream = torch._C._cuda_getCurrentRawStream(device)
+    if torch._C._cuda_getDevice() == device:
+        rc = fn(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, stream)
+    if rc:
+        B.check(rc)
 
 
 def _need(ok: bool, what: str) -> None:
@@ -35,17 +44,26 @@ def _need(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
-def _ints(t: torch.Tensor, shape, what: str) -> int:
-    if t.dtype is not torch.int32 or t.shape != shape or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{what}: a contiguous int32 tensor {tuple(shape)} on the GPU is needed, got {t.dtype} {tuple(t.shape)} on {t.device}")
+def _index(t: torch.Tensor) -> int:
+    """The GPU that a tensor is on, -2 for none: what other tensors are compared with."""
+    return t.get_device() if t.is_cuda else -2
+
+
+def _ints(t: torch.Tensor, shape, device: int, what: str) -> int:
+    if t.dtype is not torch.int32 or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous int32 tensor {tuple(shape)} on {_gpu(device)} is needed, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _rows(t: torch.Tensor, shape, dtype, what: str) -> Tuple[int, int]:
+def _gpu(device: int) -> str:
+    return f"GPU {device}" if device >= 0 else "the GPU"
+
+
+def _rows(t: torch.Tensor, shape, dtype, device: int, what: str) -> Tuple[int, int]:
     """(pointer, elements between rows) of [n][heads][dim] whose heads follow each other."""
     n, heads, dim = shape
-    if t.dtype is not dtype or t.shape != shape or not t.is_cuda:
-        raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)} on {t.device}, {dtype} {shape} on the GPU is needed")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
+        raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)} on {t.device}, {dtype} {shape} on {_gpu(device)} is needed")
     row, head, one = t.stride()
     if one != 1 or (head != dim and heads != 1):
         raise ValueError(f"{what}: the heads of a row have to follow each other")
@@ -70,6 +88,7 @@ class Cache:
         self.n_pages, self.kv_heads, self.page, self.head_dim = p, h, 16 * s, 16 * d
         self.c = B.KvCache(p, 16 * s, h, 16 * d, FORMATS[k.dtype], 0, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
         self.ref = C.byref(self.c)
+        self.device = _index(k)
 
     @classmethod
     def empty(cls, n_pages: int, kv_heads: int, head_dim: int, page: int = 64, dtype=torch.float8_e4m3fn, device="cuda:0") -> "Cache":
@@ -95,6 +114,7 @@ class Step:
         self.row_start, self.positions, self.slots = i32(n_requests + 1), i32(n_tokens), i32(n_tokens)
         self.kv_len, self.status, self.free_left = i32(n_requests), i32(n_requests), i32(1)
         self.plan_dev = torch.empty(n, dtype=torch.uint8, device=device)
+        self.device = _index(self.plan_dev)
         self.scratch_bytes = B.moe_kv_scratch_bytes(self.s)
         self.scratch = torch.empty(max(16, self.scratch_bytes), dtype=torch.uint8, device=device)
         self.block_table: Optional[torch.Tensor] = None
@@ -108,14 +128,12 @@ class Step:
     def plan(self, ctx_len, new_len, block_table, free_pages, free_count) -> None:
         """Pages for the step's new tokens (block_table is updated in place, ctx_len and the stack stay until `advance`).
         A free_count above the length of free_pages counts as that length."""
-        x = self._lists
-        x.ctx_len, x.new_len = _ints(ctx_len, self._per_request, "ctx_len"), _ints(new_len, self._per_request, "new_len")
-        x.block_table = _ints(block_table, self._table, "block_table")
+        x, at = self._lists, self.device
+        x.ctx_len, x.new_len = _ints(ctx_len, self._per_request, at, "ctx_len"), _ints(new_len, self._per_request, at, "new_len")
+        x.block_table = _ints(block_table, self._table, at, "block_table")
         _need(free_pages.dim() == 1 and free_pages.numel() >= 1, "plan: free_pages is a list")
-        x.free_pages, x.free_count = _ints(free_pages, free_pages.shape, "free_pages"), _ints(free_count, (1,), "free_count")
-        rc = B.lib().moe_kv_plan_within(self._ref, self._lists_ref, free_pages.numel(), self.plan_dev.data_ptr(), _stream(self.plan_dev))
-        if rc:
-            B.check(rc)
+        x.free_pages, x.free_count = _ints(free_pages, free_pages.shape, at, "free_pages"), _ints(free_count, (1,), at, "free_count")
+        _call(B.lib().moe_kv_plan_within, at, self._ref, self._lists_ref, free_pages.numel(), self.plan_dev.data_ptr())
         self.block_table, self._ctx, self._count = block_table, ctx_len, free_count
 
     def advance(self) -> None:
@@ -132,33 +150,33 @@ def write(cache: Cache, step: Step, q: torch.Tensor, k: torch.Tensor, v: torch.T
     the cache.  q [n_tokens, q_heads, head_dim], k, v [n_tokens, kv_heads, head_dim], views of one packed tensor among them.
     Returns the queries: q_out (which may be q), a new tensor if it is None; rows that belong to no request are left as they are."""
     _need(step.block_table is not None, "write: the step has no plan yet")
-    dtype, x = q.dtype, step._row
+    dtype, x, at = q.dtype, step._row, step.device
     if dtype not in DTYPES:
         raise ValueError(f"write: queries of type {dtype}")
+    if cache.device != at:
+        raise ValueError(f"write: the cache is on {_gpu(cache.device)}, the step on {_gpu(at)}")
     if q_out is None:
         q_out = torch.empty(step._q_shape, dtype=dtype, device=q.device)
-    x.q, x.q_stride = _rows(q, step._q_shape, dtype, "q")
-    x.q_out, x.q_out_stride = _rows(q_out, step._q_shape, dtype, "q_out")
-    x.k, x.k_stride = _rows(k, step._kv_shape, dtype, "k")
-    x.v, x.v_stride = _rows(v, step._kv_shape, dtype, "v")
+    x.q, x.q_stride = _rows(q, step._q_shape, dtype, at, "q")
+    x.q_out, x.q_out_stride = _rows(q_out, step._q_shape, dtype, at, "q_out")
+    x.k, x.k_stride = _rows(k, step._kv_shape, dtype, at, "k")
+    x.v, x.v_stride = _rows(v, step._kv_shape, dtype, at, "v")
     x.dtype, x.eps, x.interleaved = DTYPES[dtype], eps, interleaved
     x.q_gamma, x.k_gamma = _gain(q_gamma, step, eps, dtype, "q_gamma"), _gain(k_gamma, step, eps, dtype, "k_gamma")
     x.rot_dim, x.inv_freq = 0, None
     if inv_freq is not None and inv_freq.numel():
-        if inv_freq.dtype is not torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous() or not inv_freq.is_cuda:
-            raise ValueError("write: inv_freq is a contiguous fp32 list on the GPU")
+        if inv_freq.dtype is not torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous() or inv_freq.get_device() != at:
+            raise ValueError(f"write: inv_freq is a contiguous fp32 list on {_gpu(at)}")
         x.rot_dim, x.inv_freq = 2 * inv_freq.numel(), inv_freq.data_ptr()
-    rc = B.lib().moe_kv_write(cache.ref, step._ref, step.plan_dev.data_ptr(), step._row_ref, _stream(q))
-    if rc:
-        B.check(rc)
+    _call(B.lib().moe_kv_write, at, cache.ref, step._ref, step.plan_dev.data_ptr(), step._row_ref)
     return q_out
 
 
 def _gain(g: Optional[torch.Tensor], step: Step, eps: float, dtype, what: str) -> Optional[int]:
     if g is None:
         return None
-    if g.shape != step._q_shape[2:] or g.dtype is not dtype or not g.is_contiguous() or not g.is_cuda:
-        raise ValueError(f"write: {what}: {step._q_shape[2]} contiguous numbers of type {dtype} are needed")
+    if g.shape != step._q_shape[2:] or g.dtype is not dtype or not g.is_contiguous() or g.get_device() != step.device:
+        raise ValueError(f"write: {what}: {step._q_shape[2]} contiguous numbers of type {dtype} on {_gpu(step.device)} are needed")
     _need(eps > 0, "write: a gain without a norm (eps is 0)")
     return g.data_ptr()
 
@@ -168,19 +186,19 @@ def attend(cache: Cache, step: Step, q: torch.Tensor, scale: Optional[float] = N
     q_heads, head_dim], or (out, lse [n_tokens, q_heads] fp32); rows that belong to no request are left as they are."""
     table = step.block_table
     _need(table is not None, "attend: the step has no plan yet")
-    dtype, x = q.dtype, step._query
+    dtype, x, at = q.dtype, step._query, step.device
     if dtype not in DTYPES:
         raise ValueError(f"attend: queries of type {dtype}")
+    if cache.device != at:
+        raise ValueError(f"attend: the cache is on {_gpu(cache.device)}, the step on {_gpu(at)}")
     if out is None:
         out = torch.empty(step._q_shape, dtype=dtype, device=q.device)
     lse = torch.empty(step._q_shape[:2], dtype=torch.float32, device=q.device) if with_lse else None
-    x.q, x.q_stride = _rows(q, step._q_shape, dtype, "q")
-    x.out, x.out_stride = _rows(out, step._q_shape, dtype, "out")
+    x.q, x.q_stride = _rows(q, step._q_shape, dtype, at, "q")
+    x.out, x.out_stride = _rows(out, step._q_shape, dtype, at, "out")
     x.dtype, x.scale, x.lse = DTYPES[dtype], step._scale if scale is None else scale, lse.data_ptr() if with_lse else None
-    rc = B.lib().moe_kv_attend(cache.ref, step._ref, step.plan_dev.data_ptr(), table.data_ptr(), step._query_ref, step.scratch.data_ptr(),
-                               step.scratch_bytes, _stream(q))
-    if rc:
-        B.check(rc)
+    _call(B.lib().moe_kv_attend, at, cache.ref, step._ref, step.plan_dev.data_ptr(), table.data_ptr(), step._query_ref, step.scratch.data_ptr(),
+          step.scratch_bytes)
     return (out, lse) if with_lse else out
 
 
@@ -189,12 +207,10 @@ def gather(cache: Cache, slots: torch.Tensor, dtype=torch.float16) -> Tuple[torc
     if dtype not in DTYPES:
         raise ValueError(f"gather: values of type {dtype}")
     _need(slots.dim() == 1, "gather: slots is a list")
-    p, n = _ints(slots, slots.shape, "slots"), slots.numel()
+    p, n = _ints(slots, slots.shape, cache.device, "slots"), slots.numel()
     k = torch.empty(n, cache.kv_heads, cache.head_dim, dtype=dtype, device=slots.device)
     v = torch.empty_like(k)
-    rc = B.lib().moe_kv_gather(cache.ref, p, n, DTYPES[dtype], k.data_ptr(), v.data_ptr(), _stream(slots))
-    if rc:
-        B.check(rc)
+    _call(B.lib().moe_kv_gather, cache.device, cache.ref, p, n, DTYPES[dtype], k.data_ptr(), v.data_ptr())
     return k, v
 
 
@@ -203,6 +219,7 @@ def release(requests: torch.Tensor, n_pages: int, page: int, ctx_len: torch.Tens
     """Give back the pages of the requests whose ids `requests` holds; their ctx_len becomes 0."""
     _need(requests.dim() == 1 and block_table.dim() == 2 and free_pages.dim() == 1, "release: requests and free_pages are lists, block_table a table")
     r, m = block_table.shape
-    B.moe_kv_release(_ints(requests, requests.shape, "requests"), requests.numel(), r, n_pages, page, m, _ints(ctx_len, (r,), "ctx_len"),
-                     _ints(block_table, (r, m), "block_table"), _ints(free_pages, free_pages.shape, "free_pages"), free_pages.numel(),
-                     _ints(free_count, (1,), "free_count"), _stream(block_table))
+    at = _index(block_table)
+    _call(B.lib().moe_kv_release, at, _ints(requests, requests.shape, at, "requests"), requests.numel(), r, n_pages, page, m, _ints(ctx_len, (r,), at, "ctx_len"),
+          _ints(block_table, (r, m), at, "block_table"), _ints(free_pages, free_pages.shape, at, "free_pages"), free_pages.numel(),
+          _ints(free_count, (1,), at, "free_count"))
