@@ -11,6 +11,7 @@ block's output is fed back as.  Prints one JSON object.  Needs a GPU and the bui
 from __future__ import annotations
 
 import argparse
+import contextlib
 import json
 import os
 import sys
@@ -29,7 +30,8 @@ from paper_2312_17238_amd.engine import Stack, layer_config  # noqa: E402
 
 
 class Decoder:
-    """`layers` blocks over a pool of `n_requests` requests.  Everything runs on the engine's compute stream."""
+    """`layers` blocks over a pool of `n_requests` requests.  Everything runs on the engine's compute stream, behind what the caller's current
+    stream has been given so far; that stream waits for the results."""
 
     def __init__(self, layers: int, hidden: int, ffn: int, q_heads: int, kv_heads: int, head_dim: int, n_requests: int, max_len: int,
                  max_rows: int, page: int = 64, fmt=torch.float8_e4m3fn, window: int = 0, eps: float = 1e-5, theta: float = 1e6,
@@ -59,8 +61,22 @@ class Decoder:
 
     def bounds(self, rows: int, most: int) -> paged.Step:
         """The workspaces of steps of `rows` rows in all and at most `most` of a request; made once for many steps."""
-        return paged.Step(self.n_requests, rows, most, self.max_blocks, self.n_pages, self.page, self.q_heads, self.kv_heads, self.head_dim,
-                          window=self.window, device=self.device)
+        with torch.cuda.stream(self.stack.compute):     # memory of the stream that uses it: it may be dropped while a step runs
+            return paged.Step(self.n_requests, rows, most, self.max_blocks, self.n_pages, self.page, self.q_heads, self.kv_heads, self.head_dim,
+                              window=self.window, device=self.device)
+
+    @contextlib.contextmanager
+    def _on_compute(self, *tensors: torch.Tensor):
+        """The compute stream, behind the caller's, which then waits for it; `tensors` of the caller's are used there."""
+        caller, compute = torch.cuda.current_stream(self.stack.device), self.stack.compute
+        compute.wait_stream(caller)
+        for t in tensors:
+            t.record_stream(compute)
+        try:
+            with torch.cuda.stream(compute):
+                yield caller
+        finally:
+            caller.wait_stream(compute)
 
     def attention_half(self, layer: int, step: paged.Step, x: torch.Tensor) -> torch.Tensor:
         """x + attention(norm(x)) Wo for the step's rows [rows, hidden]."""
@@ -74,7 +90,7 @@ class Decoder:
 
     def step(self, step: paged.Step, x: torch.Tensor, new: Optional[Sequence[int]] = None) -> torch.Tensor:
         """One step of all blocks for rows x [rows, hidden] (fp16); new: tokens of each request if they changed since the last step."""
-        with torch.cuda.stream(self.stack.compute):
+        with self._on_compute(x) as caller:
             if new is not None:
                 self.new_len.copy_(torch.tensor(new, dtype=torch.int32))
             step.plan(self.ctx_len, self.new_len, self.block_table, self.free_pages, self.free_count)
@@ -84,11 +100,12 @@ class Decoder:
                 self.stack.step_layer(l, x, out)
                 x = out
             step.advance()
+            x.record_stream(caller)
         return x
 
     def finish(self, requests: List[int]) -> None:
         """The requests' pages go back to the pool."""
-        with torch.cuda.stream(self.stack.compute):
+        with self._on_compute():
             ids = torch.tensor(requests, dtype=torch.int32).to(self.device)
             paged.release(ids, self.n_pages, self.page, self.ctx_len, self.block_table, self.free_pages, self.free_count)
 
@@ -108,10 +125,8 @@ def main(argv=None) -> dict:
     d = Decoder(a.layers, a.hidden, a.ffn, a.q_heads, a.kv_heads, a.head_dim, a.requests, a.prompt + a.tokens, max(rows, a.requests), a.page,
                 torch.float8_e4m3fn if a.format == "e4m3" else torch.int8, a.window, cache_slots=a.cache_slots, seed=a.seed)
     x = W.hidden_ar1(a.seed, 1, rows, a.hidden)[0].to(d.device)
-    torch.cuda.synchronize()
     x = d.step(d.bounds(rows, max(prompts)), x, prompts)
     ends = torch.tensor(prompts).cumsum(0) - 1
-    d.stack.synchronize()
     x = x[ends.to(d.device)].contiguous()
     one = d.bounds(a.requests, 1)
     x = d.step(one, x, [1] * a.requests)
