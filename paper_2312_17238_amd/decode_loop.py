@@ -35,11 +35,13 @@ class Decoder:
 
     def __init__(self, layers: int, hidden: int, ffn: int, q_heads: int, kv_heads: int, head_dim: int, n_requests: int, max_len: int,
                  max_rows: int, page: int = 64, fmt=torch.float8_e4m3fn, window: int = 0, eps: float = 1e-5, theta: float = 1e6,
-                 cache_slots: int = 8, seed: int = 0, device: str = "cuda:0"):
+                 cache_slots: int = 8, seed: int = 0, device: str = "cuda:0", n_pages: Optional[int] = None):
         self.layers, self.hidden, self.q_heads, self.kv_heads, self.head_dim = layers, hidden, q_heads, kv_heads, head_dim
         self.n_requests, self.page, self.window, self.eps, self.device = n_requests, page, window, eps, device
         self.max_blocks = -(-max_len // page)
-        self.n_pages = n_requests * self.max_blocks
+        self.n_pages = n_requests * self.max_blocks if n_pages is None else n_pages
+        # The host makes the lengths, so it knows them without reading any: tokens and new tokens of each request, free pages, rows of a step.
+        self._lens, self._new, self._free, self._rows = [0] * n_requests, [0] * n_requests, self.n_pages, 0
         cfg = layer_config(hidden, ffn, 8, 2, 4, 64, cache_slots, 2 if cache_slots < 8 else 0, eps, 1 if cache_slots == 8 else 0)
         self.stack = Stack([cfg] * layers, [W.gate_weight(seed, l, 8, hidden) for l in range(layers)], [W.rms_gamma(hidden)] * layers,
                            n_staging=0 if cache_slots == 8 else 4, max_batch=max_rows, device=device)
@@ -85,21 +87,44 @@ class Decoder:
         h = (f * torch.rsqrt(f.square().mean(-1, keepdim=True) + self.eps)).half()
         qkv = (h @ self.wqkv[layer]).view(-1, hq + 2 * hk, d)
         q = paged.write(self.caches[layer], step, qkv[:, :hq], qkv[:, hq:hq + hk], qkv[:, hq + hk:], inv_freq=self.inv_freq, q_out=qkv[:, :hq])
-        a = paged.attend(self.caches[layer], step, q)
+        # rows of no request are left alone by attention
+        a = paged.attend(self.caches[layer], step, q, out=None if self._rows == len(x) else x.new_zeros(len(x), hq, d))
         return x + a.view(-1, hq * d) @ self.wo[layer]
 
+    def _pages(self, tokens: int) -> int:
+        return -(-tokens // self.page)
+
+    def _check(self, step: paged.Step, new: List[int]) -> None:
+        """Raises if the step would turn a request down, whose hidden state would go on without its token."""
+        if len(new) != self.n_requests or min(new) < 0 or max(new) > step.s.max_new or sum(new) > step.s.n_tokens:
+            raise ValueError(f"Decoder: {new} new tokens of {self.n_requests} requests do not fit a step of {step.s.n_tokens} rows, {step.s.max_new} of a request")
+        for r, (c, n) in enumerate(zip(self._lens, new)):
+            if n and self._pages(c + n) > self.max_blocks:
+                raise ValueError(f"Decoder: request {r} has {c} tokens, {n} more are beyond {self.max_blocks} pages of {self.page}")
+        need = sum(self._pages(c + n) - self._pages(c) for c, n in zip(self._lens, new))
+        if need > self._free:
+            raise ValueError(f"Decoder: {need} more pages are needed, {self._free} are free")
+
     def step(self, step: paged.Step, x: torch.Tensor, new: Optional[Sequence[int]] = None) -> torch.Tensor:
-        """One step of all blocks for rows x [rows, hidden] (fp16); new: tokens of each request if they changed since the last step."""
+        """One step of all blocks for rows x [rows, hidden] (fp16); new: tokens of each request if they changed since the last step.  Rows past
+        the requests' tokens come back as they are.  A step that cannot serve every request is refused (ValueError) before anything runs."""
+        now = self._new if new is None else list(new)
+        self._check(step, now)
         with self._on_compute(x) as caller:
             if new is not None:
-                self.new_len.copy_(torch.tensor(new, dtype=torch.int32))
+                self.new_len.copy_(torch.tensor(now, dtype=torch.int32))
+            self._new, self._rows = now, sum(now)
             step.plan(self.ctx_len, self.new_len, self.block_table, self.free_pages, self.free_count)
-            for l in range(self.layers):
+            for l in range(self.layers if self._rows else 0):
                 x = self.attention_half(l, step, x)
                 out = torch.empty_like(x)
-                self.stack.step_layer(l, x, out)
+                self.stack.step_layer(l, x[:self._rows], out[:self._rows])      # the others take no expert
+                if self._rows < len(x):
+                    out[self._rows:] = x[self._rows:]
                 x = out
             step.advance()
+            self._free -= sum(self._pages(c + n) - self._pages(c) for c, n in zip(self._lens, now))
+            self._lens = [c + n for c, n in zip(self._lens, now)]
             x.record_stream(caller)
         return x
 
@@ -108,6 +133,10 @@ class Decoder:
         with self._on_compute():
             ids = torch.tensor(requests, dtype=torch.int32).to(self.device)
             paged.release(ids, self.n_pages, self.page, self.ctx_len, self.block_table, self.free_pages, self.free_count)
+        for r in requests:
+            if 0 <= r < self.n_requests:
+                self._free += self._pages(self._lens[r])
+                self._lens[r] = 0
 
     def close(self) -> None:
         self.stack.close()
