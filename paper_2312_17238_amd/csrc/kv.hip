@@ -184,8 +184,9 @@ extern "C" int32_t moe_kv_release(const int32_t *requests, int32_t n, int32_t n_
                                   int32_t *free_count, void *stream)
 {
     if (n < 0 || n_requests < 1 || max_blocks < 1 || capacity < 1 || !geometry_ok(n_pages, page, 1, 64)) return bad("moe_kv_release: a bad size");
-    if (!requests || !ctx_len || !block_table || !free_pages || !free_count) return bad("moe_kv_release: a null list");
     if (n == 0) return MOE_OK;
+    for (const void *p : {(const void *)requests, (const void *)ctx_len, (const void *)block_table, (const void *)free_pages, (const void *)free_count})
+        if (!p || ((uintptr_t)p & 3)) return bad("moe_kv_release: a null or misaligned list");
     hipLaunchKernelGGL(k_kv_release, dim3(1), dim3(256), 0, static_cast<hipStream_t>(stream), requests, n, n_requests, n_pages, page, max_blocks, ctx_len, block_table,
                        free_pages, capacity, free_count);
     return launched("moe_kv_release");

@@ -25,3 +25,9 @@ def test_nothing_behind_the_free_list_is_handed_out(count):
     start, positions, slots, kv, status, left = lists
     assert step.status.tolist() == status and step.free_left.tolist() == [left] and step.slots.tolist() == slots and step.kv_len.tolist() == kv
     assert table.tolist() == want.tolist() and not (set(table.flatten().tolist()) & set(range(8)))
+
+
+def test_giving_back_nothing():
+    table, ctx, free, count = i32([[3, 4]]), i32([20]), i32([0, 1, -7, -7]), i32([2])
+    paged.release(i32([]), 8, 16, ctx, table, free, count)
+    assert ctx.tolist() == [20] and count.tolist() == [2] and free.tolist() == [0, 1, -7, -7]

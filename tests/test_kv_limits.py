@@ -25,3 +25,14 @@ def test_a_stack_without_room_is_refused(room):
     with pytest.raises(B.MoeError, match="moe_kv_plan") as e:
         B.moe_kv_plan_within(step, lists, room, at, 0)
     assert e.value.code == B.MOE_EINVAL
+
+
+def test_giving_back_nothing_is_no_error():
+    """An empty list has no address."""
+    at = 0x10000
+    B.moe_kv_release(0, 0, 4, 32, 16, 8, at, at, at, 32, at, 0)
+    for i in (0, 6, 7, 8, 10):
+        args = [at, 1, 4, 32, 16, 8, at, at, at, 32, at, 0]
+        args[i] += 2
+        with pytest.raises(B.MoeError, match="moe_kv_release"):
+            B.moe_kv_release(*args)
