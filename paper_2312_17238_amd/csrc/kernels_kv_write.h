@@ -23,6 +23,7 @@ struct WriteArgs {
     moe_kv_rows_t r;
     Plan p;
     int32_t q_heads, n_tokens;
+    int32_t first;          // block of the whole grid that this launch begins with
     int32_t kv_blocks;      // blocks that store; the others turn queries
     int32_t q_tokens;       // tokens of a query block
     int32_t heads;          // heads of a block that stores, and rows of codes that its LDS holds
@@ -151,11 +152,12 @@ __global__ void __launch_bounds__(WRITE_THREADS) k_kv_write(WriteArgs a)
     extern __shared__ __align__(16) uint8_t write_lds[];
     uint8_t *lds = write_lds;
     const bool rope = rot > 0;
+    const int block = a.first + blockIdx.x;
 
-    if ((int)blockIdx.x >= a.kv_blocks) {
+    if (block >= a.kv_blocks) {
         // ---- queries: lds holds (cos, sin) of q_tokens tokens
         float2 *cs = reinterpret_cast<float2 *>(lds);
-        const int t0 = (blockIdx.x - a.kv_blocks) * a.q_tokens;
+        const int t0 = (block - a.kv_blocks) * a.q_tokens;
         const int n = min(a.q_tokens, a.n_tokens - t0), rows = n * a.q_heads;
         // lanes past the end repeat the last head, without storing it
         auto place = [&](int r, int &t, int &h) {
@@ -190,7 +192,7 @@ __global__ void __launch_bounds__(WRITE_THREADS) k_kv_write(WriteArgs a)
     // ---- keys or values of a page, of hg heads
     const int heads = a.c.kv_heads, page = a.c.page, groups = div_up(heads, a.heads);
     constexpr bool ONE = ITER > 1;              // several passes: one head
-    const int which = blockIdx.x & 1, si = (blockIdx.x >> 1) / groups, h0 = ((blockIdx.x >> 1) - si * groups) * a.heads, hg = ONE ? 1 : min(a.heads, heads - h0);
+    const int which = block & 1, si = (block >> 1) / groups, h0 = ((block >> 1) - si * groups) * a.heads, hg = ONE ? 1 : min(a.heads, heads - h0);
     const uint32_t per_hg = ONE ? 0 : 0xFFFF / (uint32_t)hg + 1;
     auto over_hg = [&](int i) { return ONE ? i : (int)((uint32_t)i * per_hg >> 16); };     // i / hg, for i < 2048 and hg <= 32
     const Segment s = a.p.segments[si];         // in flight with the list's length
@@ -390,10 +392,11 @@ __global__ void __launch_bounds__(WRITE_THREADS) k_kv_write(WriteArgs a)
 // Sixteen entries of the list and one head.  Two waves take the keys, a token's 16 dims a thread; two the values, two dims of all
 // sixteen tokens a thread, whose pieces of sixteen tokens are loaded anew only where the next entry lies in another one.
 template <int DTYPE, int FMT>
-__global__ void __launch_bounds__(256) k_kv_gather(moe_kv_cache_t c, const int32_t *slots, int n, void *k_out, void *v_out)
+__global__ void __launch_bounds__(256) k_kv_gather(moe_kv_cache_t c, uint32_t first, const int32_t *slots, int n, void *k_out, void *v_out)
 {
     const int D = c.head_dim, page_shift = 31 - __builtin_clz(c.page), page = c.page, heads = c.kv_heads;
-    const int head = blockIdx.x % heads, e0 = (blockIdx.x / heads) * SUB, tid = threadIdx.x & 127;
+    const uint32_t block = first + blockIdx.x;      // of the whole grid
+    const int head = block % heads, e0 = (block / heads) * SUB, tid = threadIdx.x & 127;
     const int m = min(SUB, n - e0);
     const uint32_t limit = (uint32_t)c.n_pages * page;
     const int mine = slots[min(e0 + (int)(threadIdx.x & 15), n - 1)];

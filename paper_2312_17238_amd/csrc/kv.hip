@@ -192,6 +192,15 @@ extern "C" int32_t moe_kv_release(const int32_t *requests, int32_t n, int32_t n_
     return launched("moe_kv_release");
 }
 
+// A launch has fewer than 2^32 threads: `launch(first, blocks)` for pieces of a grid of blocks of 256.
+constexpr int64_t MOST_BLOCKS = (1ll << 24) - 1;
+
+template <class F>
+static void in_pieces(int64_t blocks, F launch)
+{
+    for (int64_t first = 0; first < blocks; first += MOST_BLOCKS) launch((uint32_t)first, (unsigned)std::min(MOST_BLOCKS, blocks - first));
+}
+
 static bool rows16(const void *p, int64_t stride) { return !((uintptr_t)p & 15) && stride % 8 == 0; }
 
 template <int DTYPE, int FMT>
@@ -244,19 +253,20 @@ extern "C" int32_t moe_kv_write(const moe_kv_cache_t *cache, const moe_kv_step_t
     // queries that neither turn nor move need no block
     const bool turn = r.rot_dim || r.eps > 0.f || r.q != r.q_out;
     const int64_t blocks = (int64_t)z.p.max_segments * div_up(cache->kv_heads, a.heads) * 2 + (turn ? div_up(step->n_tokens, a.q_tokens) : 0);
-    if (blocks > 0x7FFFFFFF) return bad("moe_kv_write: too many blocks");
     const size_t lds = std::max<size_t>((size_t)a.lds_rows * (D + 16) + per_pass * angles, (size_t)a.q_tokens * angles);
     int iter = 1;
     while (iter * per_pass < a.lds_rows) iter *= 2;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    const dim3 grid((unsigned)blocks);
-    if (r.dtype == MOE_KV_F16) {
-        if (cache->format == MOE_KV_E4M3) launch_write<MOE_KV_F16, MOE_KV_E4M3>(a, iter, grid, lds, s);
-        else launch_write<MOE_KV_F16, MOE_KV_INT8>(a, iter, grid, lds, s);
-    } else {
-        if (cache->format == MOE_KV_E4M3) launch_write<MOE_KV_BF16, MOE_KV_E4M3>(a, iter, grid, lds, s);
-        else launch_write<MOE_KV_BF16, MOE_KV_INT8>(a, iter, grid, lds, s);
-    }
+    in_pieces(blocks, [&](uint32_t first, unsigned n) {
+        a.first = (int32_t)first;
+        if (r.dtype == MOE_KV_F16) {
+            if (cache->format == MOE_KV_E4M3) launch_write<MOE_KV_F16, MOE_KV_E4M3>(a, iter, dim3(n), lds, s);
+            else launch_write<MOE_KV_F16, MOE_KV_INT8>(a, iter, dim3(n), lds, s);
+        } else {
+            if (cache->format == MOE_KV_E4M3) launch_write<MOE_KV_BF16, MOE_KV_E4M3>(a, iter, dim3(n), lds, s);
+            else launch_write<MOE_KV_BF16, MOE_KV_INT8>(a, iter, dim3(n), lds, s);
+        }
+    });
     return launched("moe_kv_write");
 }
 
@@ -312,8 +322,8 @@ extern "C" int32_t moe_kv_attend(const moe_kv_cache_t *cache, const moe_kv_step_
     a.sub_shift = log2_of(cache->page / SUB);
     a.vec_q = rows16(q.q, q.q_stride);
     a.vec_out = rows16(q.out, q.out_stride);
+    // below 2^24: a million rows of 1024 query heads are 2^23 tiles, 4096 requests of 256 heads have 2^20 more
     const int64_t many = (int64_t)z.p.max_many * cache->kv_heads, blocks = many + (int64_t)z.p.blocks_few * cache->kv_heads;
-    if (blocks > 0x7FFFFFFF) return bad("moe_kv_attend: too many blocks");
     a.many_blocks = (int32_t)many;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const dim3 grid((unsigned)blocks);
@@ -333,14 +343,16 @@ extern "C" int32_t moe_kv_gather(const moe_kv_cache_t *cache, const int32_t *slo
     if (n < 0 || n > (1 << 26) || (dtype != MOE_KV_F16 && dtype != MOE_KV_BF16)) return bad("moe_kv_gather: bad count or type");
     if (n == 0) return MOE_OK;
     if (!slots || !k_out || !v_out || (((uintptr_t)k_out | (uintptr_t)v_out) & 15) || ((uintptr_t)slots & 3)) return bad("moe_kv_gather: a null or misaligned pointer");
-    const dim3 grid((unsigned)((int64_t)div_up(n, SUB) * cache->kv_heads));
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    if (dtype == MOE_KV_F16) {
-        if (cache->format == MOE_KV_E4M3) hipLaunchKernelGGL((k_kv_gather<MOE_KV_F16, MOE_KV_E4M3>), grid, dim3(256), 0, s, *cache, slots, n, k_out, v_out);
-        else hipLaunchKernelGGL((k_kv_gather<MOE_KV_F16, MOE_KV_INT8>), grid, dim3(256), 0, s, *cache, slots, n, k_out, v_out);
-    } else {
-        if (cache->format == MOE_KV_E4M3) hipLaunchKernelGGL((k_kv_gather<MOE_KV_BF16, MOE_KV_E4M3>), grid, dim3(256), 0, s, *cache, slots, n, k_out, v_out);
-        else hipLaunchKernelGGL((k_kv_gather<MOE_KV_BF16, MOE_KV_INT8>), grid, dim3(256), 0, s, *cache, slots, n, k_out, v_out);
-    }
+    in_pieces((int64_t)div_up(n, SUB) * cache->kv_heads, [&](uint32_t first, unsigned blocks) {
+        const dim3 grid(blocks);
+        if (dtype == MOE_KV_F16) {
+            if (cache->format == MOE_KV_E4M3) hipLaunchKernelGGL((k_kv_gather<MOE_KV_F16, MOE_KV_E4M3>), grid, dim3(256), 0, s, *cache, first, slots, n, k_out, v_out);
+            else hipLaunchKernelGGL((k_kv_gather<MOE_KV_F16, MOE_KV_INT8>), grid, dim3(256), 0, s, *cache, first, slots, n, k_out, v_out);
+        } else {
+            if (cache->format == MOE_KV_E4M3) hipLaunchKernelGGL((k_kv_gather<MOE_KV_BF16, MOE_KV_E4M3>), grid, dim3(256), 0, s, *cache, first, slots, n, k_out, v_out);
+            else hipLaunchKernelGGL((k_kv_gather<MOE_KV_BF16, MOE_KV_INT8>), grid, dim3(256), 0, s, *cache, first, slots, n, k_out, v_out);
+        }
+    });
     return launched("moe_kv_gather");
 }

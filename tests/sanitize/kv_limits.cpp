@@ -64,6 +64,23 @@ int main()
             need(of_block >= MIN_KT_MANY && ((int64_t)of_block * many >= all || of_block >= steps), "share", all, of_block);
         }
     }
+    // grids: every block in one piece, no piece of 2^32 threads
+    for (int64_t blocks : {(int64_t)0, (int64_t)1, MOST_BLOCKS, MOST_BLOCKS + 1, 3 * MOST_BLOCKS - 1, (int64_t)(1 << 30) + 5}) {
+        int64_t next = 0;
+        in_pieces(blocks, [&](uint32_t first, unsigned n) {
+            need(first == next && n >= 1 && (uint64_t)n * 256 < (1ull << 32), "pieces", first, n);
+            next = (int64_t)first + n;
+        });
+        need(next == blocks, "all pieces", blocks, next);
+    }
+    // attention is one launch: its largest steps
+    for (int heads = 1; heads <= 256; heads *= 2) {
+        moe_kv_step_t s = large_step(16, 1 << 19);
+        s.kv_heads = heads;
+        const Sizes z = sizes_of(&s);
+        const int64_t blocks = ((int64_t)z.p.max_many + z.p.blocks_few) * heads;
+        need(step_ok(&s) && blocks <= MOST_BLOCKS, "blocks of the attention", heads, blocks);
+    }
     if (failures == 0) printf("ok\n");
     return failures != 0;
 }
