@@ -132,7 +132,7 @@ __device__ __forceinline__ void load_queries(const AttendArgs &a, const Item &it
 #pragma unroll
         for (int i = 0; i < D / 4; ++i) top = max(top, max(w[i] & 0x7F80, (w[i] >> 16) & 0x7F80));
         top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-        const int e = min(max((int)(top >> 7) - 127 - 14, -100), 100);
+        const int e = max((int)(top >> 7) - 127 - 14, -100);
         by = ldexpf(1.f, -e);
         unit = ldexpf(1.f, e);
     } else {

@@ -138,7 +138,7 @@ struct Decode {
             for (int i = 0; i < D / 8; ++i) top = max(top, max(x.q[i] & 0x7F80, (x.q[i] >> 16) & 0x7F80));
             top = max(top, (uint32_t)__shfl_xor((int)top, 16));
             top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-            const int e = min(max((int)(top >> 7) - 127 - 14, -100), 100);
+            const int e = max((int)(top >> 7) - 127 - 14, -100);
             by = ldexpf(1.f, -e);
             unit = ldexpf(1.f, e);
         }
