@@ -17,8 +17,8 @@
  *   v: [n_pages][kv_heads][page/16][head_dim/16][16 dims][16 tokens]
  *   value = code * scale[page][kv head]
  * Codes are finite: the store clamps numbers to +-65504 (fp16 rows) or +-2^100 (bf16 rows), infinities with them, and takes NaN for 0, for
- * a single NaN would otherwise reach every token of its page.  A scale is finite and not negative; of scales below 2^-100
- * attention takes 2^-100.
+ * a single NaN would otherwise reach every token of its page.  A scale is not negative and 2^100 at most; of scales below
+ * 2^-96, the store's least, attention takes 2^-96.
  */
 #ifndef MOE_KV_H
 #define MOE_KV_H

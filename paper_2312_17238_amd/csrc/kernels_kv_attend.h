@@ -11,8 +11,9 @@
 //
 // A lane's sixteen tokens lie in one page, hence under one scale each for keys and values.  With t = scale log2(e) ks (q.k) + log2(vs)
 // the weight of a value's code is 2^(t - m), m the running maximum of t over the row: scales cost one multiply-add a score, and
-// the weights stay below one whatever the scales are, as fp16 wants it.  The sum of the probabilities is that of the weights, divided by vs page by page,
-// in fp32 as are scores, maxima and outputs.  Weights are rounded to fp16 (2^-11 of a weight at most, as an fp16 output is);
+// the weights stay below 2^8 (see RISE) whatever the scales are, as fp16 wants it.  The sum of the probabilities is that of the weights, divided by vs page
+// by page, in fp32 as are scores, maxima and outputs; where value scales lie so far apart that a weight may be too small for fp32 and its
+// probability matter, the probabilities' exponentials are worked out for themselves (see WIDE).  Weights are rounded to fp16 (2^-11 of a weight at most, as an fp16 output is);
 // bf16 queries become fp16 after a power of two is taken off each row.
 #pragma once
 #include "kernels_kv_common.h"
@@ -85,8 +86,49 @@ template <int D>
 struct State {
     v16f o[D / 32];     // O^T: column is the lane's row, rows are dims 32 n + 8 (i/4) + 4 h + i%4
     float m, l;
-    bool big;           // of any row of the wave: |m| is so large that fp32's steps there matter to an exponent
+    bool rare;          // a value scale beyond WIDE has been met, or a row of the wave has had an |m| beyond BIG
 };
+
+// Smaller scales count as this one, the least that the store writes: sums of 2^24 probabilities, each up to 2^8 / vs, stay within fp32.
+constexpr float LEAST_SCALE = 0x1p-96f;
+
+// Value scales from 2^-WIDE to 2^WIDE are 90 powers of two apart at most: a weight below 2^-126, which the exponential takes for 0, then belongs
+// to a probability below 2^-28 of the largest (the maximum may be 8 too low).  From the first scale outside on, the sum's exponentials do without
+// the scales.  A page of zeros, whose scale is 2^-96, is such a page; other than that, values beyond 2^45 or below 2^-36 are.
+constexpr float WIDE = 45.f;
+// Where fp32's steps of a maximum matter to an exponent: m is a rounded t, the others' exponents are rounded once, after m is taken off.
+// Beyond 2^20 the difference shows in a weight, at 2^28 as one that fp16 does not hold.
+constexpr float BIG = 0x1p20f;
+
+__device__ __forceinline__ bool beyond_big(float m) { return fabsf(m) > BIG && fabsf(m) < INFINITY; }
+
+// l 2^d, d <= 0, also where 2^d is less than fp32 holds.
+__device__ __forceinline__ float times_two_to(float l, float d)
+{
+    const float f = exp2f(d), h = __builtin_amdgcn_exp2f(0.5f * d);
+    return f < 0x1p-126f ? l * h * h : l * f;
+}
+
+// The waves' sums of a row, taken to `base`.  Where a sum's power of two is below what fp32 holds is looked for, not worked out: 64
+// requests took 74.5 us instead of 73 with times_two_to alone.
+template <int WAVES, int ROWS>
+__device__ __forceinline__ float sum_of_waves(const float (&m)[WAVES][ROWS], const float (&l)[WAVES][ROWS], int row, float base)
+{
+    float sum = 0.f;
+    bool low = false;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        const float d = m[w][row] - base;
+        sum += l[w][row] * exp2f(d);
+        low |= d < -126.f && l[w][row] > 0.f;
+    }
+    if (__any(low)) {
+        sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) sum += times_two_to(l[w][row], m[w][row] - base);
+    }
+    return sum;
+}
 
 template <int D>
 __device__ __forceinline__ void clear(State<D> &s)
@@ -97,7 +139,7 @@ __device__ __forceinline__ void clear(State<D> &s)
         for (int i = 0; i < 16; ++i) s.o[n][i] = 0.f;
     s.m = -INFINITY;
     s.l = 0.f;
-    s.big = false;
+    s.rare = false;
 }
 
 // Queries of 32 rows as the second operand of the first product.  k-slot (step 2i + c, lane half h, j) stands for dim
@@ -221,25 +263,32 @@ __device__ __forceinline__ void steps(State<D> &s, const v8h (&q)[D / 16], KF kf
     if (__any(t > s.m + RISE)) {
         const float m = fmaxf(s.m, t);
         const float f = m == -INFINITY ? 1.f : exp2f(s.m - m);
-        s.l *= f;
+        s.l = m == -INFINITY ? s.l : times_two_to(s.l, s.m - m);
 #pragma unroll
         for (int n = 0; n < D / 32; ++n)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s.o[n][i] *= f;
         s.m = m;
-        s.big = __any(fabsf(m) > 0x1p20f && fabsf(m) < INFINITY);
+        s.rare |= __any(beyond_big(m));
     }
     const float base = s.m == -INFINITY ? 0.f : s.m;
 #pragma unroll
     for (int u = 0; u < N; ++u)
 #pragma unroll
         for (int i = 0; i < 16; ++i) z[u][i] = fmaf(z[u][i], sc[u], lv[u] - base);
-    // m is a rounded t, these are not: beyond 2^20 the difference shows in a weight, at 2^28 as one that fp16 does not hold
-    if (s.big) {
+    float w[N];
 #pragma unroll
-        for (int u = 0; u < N; ++u)
+    for (int u = 0; u < N; ++u) w[u] = iv[u];
+    if (s.rare) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) z[u][i] = z[u][i] > RISE ? RISE : z[u][i];
+        for (int u = 0; u < N; ++u) {
+            w[u] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                z[u][i] = z[u][i] > RISE ? RISE : z[u][i];
+                s.l += __builtin_amdgcn_exp2f(z[u][i] - lv[u]);
+            }
+        }
     }
 #pragma unroll
     for (int u = 0; u < N; ++u) {
@@ -251,7 +300,7 @@ __device__ __forceinline__ void steps(State<D> &s, const v8h (&q)[D / 16], KF kf
             sum += e;
             p[i / 8][i % 8] = (_Float16)e;
         }
-        s.l = fmaf(sum, iv[u], s.l);
+        s.l = fmaf(sum, w[u], s.l);
         // neighbouring instructions into different outputs: one into the same waits for it
 #pragma unroll
         for (int c = 0; c < 2; ++c)
@@ -286,8 +335,8 @@ __device__ __forceinline__ Place place_of(const AttendArgs &a, const Item &it, i
         const int id = a.table[(int64_t)it.req * a.max_blocks + blk];
         if ((unsigned)id < (unsigned)a.c.n_pages) {
             p.id = id;
-            p.ks = fmaxf(a.c.k_scale[(int64_t)id * a.c.kv_heads + head], 0x1p-100f);
-            p.vs = fmaxf(a.c.v_scale[(int64_t)id * a.c.kv_heads + head], 0x1p-100f);
+            p.ks = fmaxf(a.c.k_scale[(int64_t)id * a.c.kv_heads + head], LEAST_SCALE);
+            p.vs = fmaxf(a.c.v_scale[(int64_t)id * a.c.kv_heads + head], LEAST_SCALE);
         }
     }
     return p;
@@ -389,6 +438,15 @@ __device__ __forceinline__ bool all_parts_done(int32_t *count, int parts, JoinSh
     return sh.last;
 }
 
+// (m, l) of two parts of a row.
+__device__ __forceinline__ void join_sum(float &m, float &l, float m2, float l2)
+{
+    const bool up = m2 > m;
+    const float n = up ? m2 : m;
+    l = n > -INFINITY ? (up ? l2 : l) + times_two_to(up ? l : l2, (up ? m : m2) - n) : l + l2;      // the latter 0, or NaN
+    m = n;
+}
+
 // Maximum and sum of each row, into LDS; 1 to 64 lanes a row.
 __device__ __forceinline__ void join_sums(const AttendArgs &a, const Item &it, int head, const float *ml, int tile_rows, int threads, JoinShared &sh)
 {
@@ -399,14 +457,11 @@ __device__ __forceinline__ void join_sums(const AttendArgs &a, const Item &it, i
     float top = -INFINITY, l = 0.f;
     for (int p = tid % lanes; p < it.parts; p += lanes) {
         const float2 v = get2(ml, (((it.part0 + p) * heads + head) * tile_rows + r) * 8u);
-        const float n = fmaxf(top, v.x);
-        l = n > -INFINITY ? l * exp2f(top - n) + v.y * exp2f(v.x - n) : l + v.y;      // the latter 0, or NaN
-        top = n;
+        join_sum(top, l, v.x, v.y);
     }
     for (int d = lanes / 2; d > 0; d >>= 1) {
-        const float m2 = __shfl_xor(top, d), l2 = __shfl_xor(l, d), n = fmaxf(top, m2);
-        l = n > -INFINITY ? l * exp2f(top - n) + l2 * exp2f(m2 - n) : l + l2;
-        top = n;
+        const float m2 = __shfl_xor(top, d), l2 = __shfl_xor(l, d);
+        join_sum(top, l, m2, l2);
     }
     if (tid % lanes == 0 && tid / lanes < rows) {
         sh.m[r] = top == -INFINITY ? 0.f : top;
@@ -616,6 +671,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, const Item &it, 
         // No branch around a load (past the end the last step is requested again): the compiler then waits for the step it
         // needs alone, with the next one's loads in flight.
         fetch(0, k[0], v[0]);
+        s.rare |= __any(fabsf(__builtin_amdgcn_logf(mine.vs)) > WIDE);
         for (int j = 0; j < n; j += 2) {
             fetch(min(j + 1, n - 1), k[1], v[1]);
             use(j, k[0], v[0]);
@@ -634,9 +690,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, const Item &it, 
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) top = fmaxf(top, sh.m[w][col]);
     const float base = top == -INFINITY ? 0.f : top;
-    float l = 0.f;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) l += sh.l[w][col] * exp2f(sh.m[w][col] - base);
+    const float l = sum_of_waves(sh.m, sh.l, col, base);
     float f = exp2f(s.m - base);
     const bool whole = it.part < 0;
     if (whole) f = l == 0.f ? 0.f : f / l;
@@ -757,6 +811,9 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const Item &it,
             }
         };
         fetch(batch);
+        bool wide = false;
+        for (int i = lane; i < places; i += 64) wide |= fabsf(sh.place[i].lv) > WIDE;
+        s.rare |= __any(wide);
         put(batch, 0);
         __syncthreads();
         int buf = 0;

@@ -84,8 +84,8 @@ struct Decode {
     __device__ __forceinline__ void settle(Ahead<D> &x) const
     {
         const bool good = (unsigned)x.id < (unsigned)a.c.n_pages;
-        x.ks = good ? fmaxf(x.ks, 0x1p-100f) : 0.f;
-        x.vs = good ? fmaxf(x.vs, 0x1p-100f) : 1.f;
+        x.ks = good ? fmaxf(x.ks, LEAST_SCALE) : 0.f;
+        x.vs = good ? fmaxf(x.vs, LEAST_SCALE) : 1.f;
     }
 
     __device__ __forceinline__ void queries(const Item &it, Ahead<D> &x) const
@@ -166,7 +166,7 @@ struct Decode {
 #pragma unroll
         for (int n = 0; n < D / 16; ++n) o[n] = v4f{0.f, 0.f, 0.f, 0.f};
         float m = -INFINITY, l = 0.f;
-        bool big = false;
+        bool rare = false;          // as in steps()
         const int all = steps(it);
         settle(x);
         place(next, wave, after);
@@ -215,22 +215,29 @@ struct Decode {
                 const float s = max_quarters(fmaf(top, sc, lv));
                 if (__any(s > m + RISE)) {
                     const float up = fmaxf(m, s), f = up == -INFINITY ? 1.f : exp2f(m - up);
-                    l *= f;
+                    l = up == -INFINITY ? l : times_two_to(l, m - up);
 #pragma unroll
                     for (int i = 0; i < D / 16; ++i) o[i] *= f;
                     m = up;
-                    big = __any(fabsf(m) > 0x1p20f && fabsf(m) < INFINITY);
+                    rare |= __any(beyond_big(m));
                 }
                 const float off = lv - (m == -INFINITY ? 0.f : m);
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) z[t][i] = fmaf(z[t][i], sc, off);
-                if (big) {      // as in steps()
+                float iv = __builtin_amdgcn_rcpf(vs);
+                // the batch's scales are looked at behind its first product, which does not wait for them
+                if (j == 0) rare |= __any(fabsf(__builtin_amdgcn_logf(x.vs)) > WIDE);
+                if (rare) {
+                    iv = 0.f;
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) z[t][i] = z[t][i] > RISE ? RISE : z[t][i];
+                        for (int i = 0; i < 4; ++i) {
+                            z[t][i] = z[t][i] > RISE ? RISE : z[t][i];
+                            l += __builtin_amdgcn_exp2f(z[t][i] - lv);
+                        }
                 }
                 v8h p[2];
                 float sum = 0.f;
@@ -242,7 +249,7 @@ struct Decode {
                         sum += e;
                         p[t / 2][4 * (t % 2) + i] = (_Float16)e;
                     }
-                l = fmaf(sum, __builtin_amdgcn_rcpf(vs), l);
+                l = fmaf(sum, iv, l);
                 if (edge) {
                     const int lo = any_lo - tok0, hi = dead ? 0 : min(any_hi, part_hi) - tok0;
 #pragma unroll
@@ -277,9 +284,7 @@ struct Decode {
 #pragma unroll
         for (int w = 0; w < DECODE_WAVES; ++w) top = fmaxf(top, sh.m[w][col]);
         const float base = top == -INFINITY ? 0.f : top;
-        l = 0.f;
-#pragma unroll
-        for (int w = 0; w < DECODE_WAVES; ++w) l += sh.l[w][col] * exp2f(sh.m[w][col] - base);
+        l = sum_of_waves(sh.m, sh.l, col, base);
         float f = exp2f(m - base);
         const bool whole = it.part < 0;
         if (whole) f = l == 0.f ? 0.f : f / l;

@@ -47,3 +47,31 @@ def test_queries_of_any_size(lens, new, dim, size):
     out, lse = paged.attend(p.cache, s, q, scale, with_lse=True)
     assert np.isfinite(lse.cpu().numpy()).all()
     check_attend(p, s, q, out, lse, lens, new, scale, rows=6)
+
+
+@pytest.mark.parametrize("lens,new", FORMS)
+@pytest.mark.parametrize("dim,fmt", [(64, "int8"), (128, "e4m3"), (256, "int8")])
+@pytest.mark.parametrize("size", [8, 31, 60, 92])
+@pytest.mark.parametrize("order", ["zeros first", "zeros last", "every other", "any"])
+def test_values_of_any_size(lens, new, dim, fmt, size, order):
+    """Pages of zeros (scale 2^-96) beside pages of very large values, with scores of the same size: tokens of either have their share of the sum.
+    'any': scales from one to the other, at random."""
+    p = pool_of(lens, dim=dim, dtype=torch.bfloat16, fmt=fmt)
+    fill(p, lens, scales="one")
+    if order == "any":
+        e = p.rng.integers(-96, size + 1, tuple(p.cache.v_scale.shape))
+    else:
+        e = np.full(tuple(p.cache.v_scale.shape), size)
+        for r, n in enumerate(lens):
+            pages = -(-n // 16)
+            for b in range(pages):
+                if {"zeros first": b < (pages + 1) // 2, "zeros last": b >= pages // 2, "every other": b % 2 == 0}[order]:
+                    i = int(p.table[r, b])
+                    e[i] = -96
+                    p.cache.v.view(torch.uint8)[i] = 0
+    p.cache.v_scale.copy_(torch.from_numpy(np.exp2(e.astype(np.float64)).astype(np.float32)))
+    s = planned(p, lens, new)
+    q = p.rows(sum(new), 4, spread=0.0)
+    scale = 1 / math.sqrt(dim)
+    out, lse = paged.attend(p.cache, s, q, scale, with_lse=True)
+    check_attend(p, s, q, out, lse, lens, new, scale, rows=6)
