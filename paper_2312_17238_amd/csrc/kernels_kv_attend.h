@@ -355,19 +355,7 @@ __device__ __forceinline__ Spot spot_of(const AttendArgs &a, const Item &it, int
     return {(page << a.sub_shift) + (sub_block & ((1 << a.sub_shift) - 1)), p.id < 0 ? 0.f : p.ks, __builtin_amdgcn_logf(p.vs), __builtin_amdgcn_rcpf(p.vs)};
 }
 
-// Writes two or four neighbouring numbers of an output row.
-template <int DTYPE>
-__device__ __forceinline__ void store2(void *out, int64_t at, bool vec, float a, float b)
-{
-    uint16_t *p = static_cast<uint16_t *>(out) + at;
-    if (vec) {
-        *reinterpret_cast<uint32_t *>(p) = pack2<DTYPE>(a, b);
-    } else {
-        p[0] = (uint16_t)to_bits<DTYPE>(a);
-        p[1] = (uint16_t)to_bits<DTYPE>(b);
-    }
-}
-
+// Writes four neighbouring numbers of an output row.
 template <int DTYPE>
 __device__ __forceinline__ void store4(void *out, int64_t at, bool vec, float a, float b, float c, float d)
 {
@@ -482,7 +470,7 @@ __device__ __forceinline__ void join_parts(const AttendArgs &a, const Item &it, 
     const int rows = min(tile_rows, it.n_new * a.group - it.tile * tile_rows);
     int pow2 = 4;
     while (pow2 < rows) pow2 *= 2;
-    // 32 bits: about 1024 parts of all heads (see target_blocks), of at most 128 rows and 256 dims
+    // 32 bits: two parts a block and head (see target_blocks), at most 1536 of all heads, of 32 rows and 256 dims
     auto at = [&](int p, int r) { return (uint32_t)(((it.part0 + p) * heads + head) * tile_rows + r); };
     // Four dims a thread; where that leaves threads over, the parts are dealt out to groups of threads.  The loads are past the
     // caches, one or two microseconds each: the first parts' are on their way before the maxima are known.
@@ -549,6 +537,7 @@ __device__ __forceinline__ void join_tile_spans(const AttendArgs &a, const Item 
 {
     constexpr int THREADS = 64 * ATTEND_WAVES, WAVE = 8 * D, AHEAD = 16, ROUNDS = AHEAD / SPAN;
     const int tid = threadIdx.x, heads = a.c.kv_heads;
+    // 32 bits: at most 1024 parts of all heads, of 128 rows and 256 dims
     const int rows = min(ROWS, it.n_new * a.group - it.tile * ROWS), quads = div_up(rows, 32) * WAVE;
     auto row_of = [&](int e) { return e / WAVE * 32 + e % 32; };
     float m[AHEAD];
