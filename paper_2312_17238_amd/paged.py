@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+import threading
 from typing import Optional, Tuple
 
 import torch
@@ -120,6 +121,7 @@ class Step:
         self.block_table: Optional[torch.Tensor] = None
         self._lists = B.KvLists(*[None] * 5, *(t.data_ptr() for t in (self.row_start, self.positions, self.slots, self.kv_len, self.status, self.free_left)))
         self._row, self._query = B.KvRows(), B.KvQuery()
+        self._lock = threading.Lock()       # a call fills these structures in, and the interpreter's lock is off while the library reads them
         self._ref, self._lists_ref, self._row_ref, self._query_ref = (C.byref(x) for x in (self.s, self._lists, self._row, self._query))
         self._per_request, self._table = (n_requests,), (n_requests, max_blocks)
         self._q_shape, self._kv_shape = (n_tokens, q_heads, head_dim), (n_tokens, kv_heads, head_dim)
@@ -129,12 +131,13 @@ class Step:
         """Pages for the step's new tokens (block_table is updated in place, ctx_len and the stack stay until `advance`).
         A free_count above the length of free_pages counts as that length."""
         x, at = self._lists, self.device
-        x.ctx_len, x.new_len = _ints(ctx_len, self._per_request, at, "ctx_len"), _ints(new_len, self._per_request, at, "new_len")
-        x.block_table = _ints(block_table, self._table, at, "block_table")
-        _need(free_pages.dim() == 1 and free_pages.numel() >= 1, "plan: free_pages is a list")
-        x.free_pages, x.free_count = _ints(free_pages, free_pages.shape, at, "free_pages"), _ints(free_count, (1,), at, "free_count")
-        _call(B.lib().moe_kv_plan_within, at, self._ref, self._lists_ref, free_pages.numel(), self.plan_dev.data_ptr())
-        self.block_table, self._ctx, self._count = block_table, ctx_len, free_count
+        with self._lock:
+            x.ctx_len, x.new_len = _ints(ctx_len, self._per_request, at, "ctx_len"), _ints(new_len, self._per_request, at, "new_len")
+            x.block_table = _ints(block_table, self._table, at, "block_table")
+            room = free_pages.numel()
+            x.free_pages, x.free_count = _ints(free_pages, (room or 1,), at, "free_pages"), _ints(free_count, (1,), at, "free_count")
+            _call(B.lib().moe_kv_plan_within, at, self._ref, self._lists_ref, room, self.plan_dev.data_ptr())
+            self.block_table, self._ctx, self._count = block_table, ctx_len, free_count
 
     def advance(self) -> None:
         """The step is done: its tokens count as cached, its pages as taken."""
@@ -149,7 +152,8 @@ def write(cache: Cache, step: Step, q: torch.Tensor, k: torch.Tensor, v: torch.T
     """Norm (eps > 0) and rotation (inv_freq: fp32, one number a pair) of queries and keys; keys and values go into
     the cache.  q [n_tokens, q_heads, head_dim], k, v [n_tokens, kv_heads, head_dim], views of one packed tensor among them.
     Returns the queries: q_out (which may be q), a new tensor if it is None; rows that belong to no request are left as they are."""
-    _need(step.block_table is not None, "write: the step has no plan yet")
+    if step.block_table is None:
+        raise ValueError("write: the step has no plan yet")
     dtype, x, at = q.dtype, step._row, step.device
     if dtype not in DTYPES:
         raise ValueError(f"write: queries of type {dtype}")
@@ -157,18 +161,19 @@ def write(cache: Cache, step: Step, q: torch.Tensor, k: torch.Tensor, v: torch.T
         raise ValueError(f"write: the cache is on {_gpu(cache.device)}, the step on {_gpu(at)}")
     if q_out is None:
         q_out = torch.empty(step._q_shape, dtype=dtype, device=q.device)
-    x.q, x.q_stride = _rows(q, step._q_shape, dtype, at, "q")
-    x.q_out, x.q_out_stride = _rows(q_out, step._q_shape, dtype, at, "q_out")
-    x.k, x.k_stride = _rows(k, step._kv_shape, dtype, at, "k")
-    x.v, x.v_stride = _rows(v, step._kv_shape, dtype, at, "v")
-    x.dtype, x.eps, x.interleaved = DTYPES[dtype], eps, interleaved
-    x.q_gamma, x.k_gamma = _gain(q_gamma, step, eps, dtype, "q_gamma"), _gain(k_gamma, step, eps, dtype, "k_gamma")
-    x.rot_dim, x.inv_freq = 0, None
-    if inv_freq is not None and inv_freq.numel():
-        if inv_freq.dtype is not torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous() or inv_freq.get_device() != at:
-            raise ValueError(f"write: inv_freq is a contiguous fp32 list on {_gpu(at)}")
-        x.rot_dim, x.inv_freq = 2 * inv_freq.numel(), inv_freq.data_ptr()
-    _call(B.lib().moe_kv_write, at, cache.ref, step._ref, step.plan_dev.data_ptr(), step._row_ref)
+    with step._lock:
+        x.q, x.q_stride = _rows(q, step._q_shape, dtype, at, "q")
+        x.q_out, x.q_out_stride = _rows(q_out, step._q_shape, dtype, at, "q_out")
+        x.k, x.k_stride = _rows(k, step._kv_shape, dtype, at, "k")
+        x.v, x.v_stride = _rows(v, step._kv_shape, dtype, at, "v")
+        x.dtype, x.eps, x.interleaved = DTYPES[dtype], eps, interleaved
+        x.q_gamma, x.k_gamma = _gain(q_gamma, step, eps, dtype, "q_gamma"), _gain(k_gamma, step, eps, dtype, "k_gamma")
+        x.rot_dim, x.inv_freq = 0, None
+        if inv_freq is not None and inv_freq.numel():
+            if inv_freq.dtype is not torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous() or inv_freq.get_device() != at:
+                raise ValueError(f"write: inv_freq is a contiguous fp32 list on {_gpu(at)}")
+            x.rot_dim, x.inv_freq = 2 * inv_freq.numel(), inv_freq.data_ptr()
+        _call(B.lib().moe_kv_write, at, cache.ref, step._ref, step.plan_dev.data_ptr(), step._row_ref)
     return q_out
 
 
@@ -185,7 +190,8 @@ def attend(cache: Cache, step: Step, q: torch.Tensor, scale: Optional[float] = N
     """Attention of the step's rows over all that is cached for their requests (scale: 1/sqrt(head_dim) if None).  Returns out [n_tokens,
     q_heads, head_dim], or (out, lse [n_tokens, q_heads] fp32); rows that belong to no request are left as they are."""
     table = step.block_table
-    _need(table is not None, "attend: the step has no plan yet")
+    if table is None:
+        raise ValueError("attend: the step has no plan yet")
     dtype, x, at = q.dtype, step._query, step.device
     if dtype not in DTYPES:
         raise ValueError(f"attend: queries of type {dtype}")
@@ -194,11 +200,12 @@ def attend(cache: Cache, step: Step, q: torch.Tensor, scale: Optional[float] = N
     if out is None:
         out = torch.empty(step._q_shape, dtype=dtype, device=q.device)
     lse = torch.empty(step._q_shape[:2], dtype=torch.float32, device=q.device) if with_lse else None
-    x.q, x.q_stride = _rows(q, step._q_shape, dtype, at, "q")
-    x.out, x.out_stride = _rows(out, step._q_shape, dtype, at, "out")
-    x.dtype, x.scale, x.lse = DTYPES[dtype], step._scale if scale is None else scale, lse.data_ptr() if with_lse else None
-    _call(B.lib().moe_kv_attend, at, cache.ref, step._ref, step.plan_dev.data_ptr(), table.data_ptr(), step._query_ref, step.scratch.data_ptr(),
-          step.scratch_bytes)
+    with step._lock:
+        x.q, x.q_stride = _rows(q, step._q_shape, dtype, at, "q")
+        x.out, x.out_stride = _rows(out, step._q_shape, dtype, at, "out")
+        x.dtype, x.scale, x.lse = DTYPES[dtype], step._scale if scale is None else scale, lse.data_ptr() if with_lse else None
+        _call(B.lib().moe_kv_attend, at, cache.ref, step._ref, step.plan_dev.data_ptr(), table.data_ptr(), step._query_ref, step.scratch.data_ptr(),
+              step.scratch_bytes)
     return (out, lse) if with_lse else out
 
 

@@ -1,6 +1,8 @@
 """Which GPU the tensor layer of the paged cache runs on, and that all tensors of a call have to be there: with tensors that only say
 that they are on a GPU, and a library that only notes how it was called."""
 import contextlib
+import threading
+import time
 
 import pytest
 import torch
@@ -97,3 +99,48 @@ def test_tensors_of_two_gpus_are_refused(machine, name, what, gpu, other):
     with pytest.raises(ValueError):
         calls(step, x)[name]()
     assert not library.calls
+
+
+def test_two_threads_may_use_one_step(machine, monkeypatch):
+    """The library reads a call's pointers while the interpreter's lock is off: another thread's call must not change them meanwhile."""
+    step, _ = machine
+    step.device = 0
+    seen = {"plan": [], "write": [], "attend": []}
+
+    class Slow:
+        @staticmethod
+        def moe_kv_plan_within(s, lists, room, plan, stream):
+            a = lists._obj.ctx_len
+            time.sleep(0.0005)
+            seen["plan"].append((a, lists._obj.free_count))
+            return 0
+
+        @staticmethod
+        def moe_kv_write(c, s, plan, rows, stream):
+            a = rows._obj.q
+            time.sleep(0.0005)
+            seen["write"].append((a, rows._obj.inv_freq))
+            return 0
+
+        @staticmethod
+        def moe_kv_attend(c, s, plan, table, query, scratch, n, stream):
+            a = query._obj.q
+            time.sleep(0.0005)
+            seen["attend"].append((a, query._obj.out))
+            return 0
+    monkeypatch.setattr(paged.B, "lib", lambda: Slow)
+    mine = [inputs(0) for _ in range(4)]
+    calls(step, mine[0])["plan"]()
+    seen["plan"].clear()
+
+    def work(x):
+        for _ in range(25):
+            for name in seen:
+                calls(step, x)[name]()
+    threads = [threading.Thread(target=work, args=(x,)) for x in mine]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for name, (a, b) in {"plan": ("ctx", "count"), "write": ("q", "freq"), "attend": ("q", "out")}.items():
+        assert sorted(seen[name]) == sorted([(x[a].data_ptr(), x[b].data_ptr()) for x in mine] * 25), name
