@@ -470,7 +470,7 @@ __device__ __forceinline__ void join_parts(const AttendArgs &a, const Item &it, 
     const int rows = min(tile_rows, it.n_new * a.group - it.tile * tile_rows);
     int pow2 = 4;
     while (pow2 < rows) pow2 *= 2;
-    // 32 bits: two parts a block and head (see target_blocks), at most 1536 of all heads, of 32 rows and 256 dims
+    // 32 bits: two parts a block and head (see target_blocks), at most 1024 of all heads, of 32 rows and 256 dims
     auto at = [&](int p, int r) { return (uint32_t)(((it.part0 + p) * heads + head) * tile_rows + r); };
     // Four dims a thread; where that leaves threads over, the parts are dealt out to groups of threads.  The loads are past the
     // caches, one or two microseconds each: the first parts' are on their way before the maxima are known.

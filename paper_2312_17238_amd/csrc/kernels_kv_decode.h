@@ -22,8 +22,9 @@ constexpr int ROWS_DECODE = 16;
 constexpr int DECODE_WAVES = 4;
 
 // Blocks of a compute unit, by their registers.  D = 128, one over 131000 and 64 over 500 to 8000: with one block 47 and 72 us, two 49
-// and 69, three (fewer registers: an item's loads no longer ahead) 67 and 92.
-__host__ __device__ constexpr int decode_blocks(int head_dim) { return head_dim == 64 ? 3 : head_dim == 128 ? 2 : 1; }
+// and 69, three (fewer registers: an item's loads no longer ahead) 67 and 92.  D = 64: with two 29.9 and 42.5, three (whose registers spill) 36.9
+// and 46.2, 512 over 300 39.1 and 50.9; D = 256 has registers for one.
+__host__ __device__ constexpr int decode_blocks(int head_dim) { return head_dim <= 128 ? 2 : 1; }
 
 template <int D>
 struct DecodeShared {

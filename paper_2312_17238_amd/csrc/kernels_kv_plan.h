@@ -241,7 +241,7 @@ __global__ void __launch_bounds__(THREADS) k_kv_plan(PlanArgs a)
         // Tiles of 32 rows, one after the other on a line of steps (a tile that sees nothing takes one step of it), cut into blocks of
         // `chunk` steps.  Either every block gets a piece of the line of the same length, whatever tiles begin and end in it; or
         // each tile begins with a block of its own (its end is padded to a whole chunk), where there are blocks enough for that: see own_chunk.
-        // Sums, and what is added to them to round up, stay below 2^32: 8192 tiles of less than 2^19 steps, or 768 blocks of as many.
+        // Sums, and what is added to them to round up, stay below 2^32: 8192 tiles of less than 2^19 steps, or 512 blocks of as many.
         constexpr int TILES = FEW_MOST / ROWS_FEW;
         int tiles[PER], kt0[PER][TILES], kt1[PER][TILES];
         uint32_t steps = 0, line, longest = 0, n_tiles = 0, all_tiles;

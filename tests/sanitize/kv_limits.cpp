@@ -52,7 +52,7 @@ int main()
         need((int64_t)lo * page >= (1 << 24) - 128, "a table narrower than it has to be", page, lo);
         // requests of few rows, all with every token that the table can name
         const int64_t steps = ((int64_t)lo * page + KT - 1) / KT;
-        const int64_t tiles = (int64_t)MOE_KV_MAX_REQUESTS * (FEW_MOST / ROWS_FEW), target = 3 * COMPUTE_UNITS;
+        const int64_t tiles = (int64_t)MOE_KV_MAX_REQUESTS * (FEW_MOST / ROWS_FEW), target = 2 * COMPUTE_UNITS;
         need(steps * tiles + target <= 1ll << 32, "the line of steps leaves 32 bits", page, steps * tiles + target);
         const uint32_t chunk = first_chunk((uint32_t)std::min<int64_t>(steps * tiles, 0xFFFFFFFF), (uint32_t)tiles, (uint32_t)target);
         need(steps * tiles <= (int64_t)chunk * target, "more blocks than there is room for", page, chunk);
