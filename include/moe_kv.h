@@ -19,6 +19,12 @@
  * Codes are finite: the store clamps numbers to +-65504 (fp16 rows) or +-2^100 (bf16 rows), infinities with them, and takes NaN for 0, for
  * a single NaN would otherwise reach every token of its page.  A scale is not negative and 2^100 at most; of scales below
  * 2^-96, the store's least, attention takes 2^-96.
+ *
+ * Whose pages these are.  A page that gets tokens belongs to one request: two whose tables name the same begun page would both rewrite
+ * it.  Full pages that several requests read may be in several tables; before a request is released, its entries of pages that
+ * others still read become -1.  Tokens are taken back by lowering ctx_len as long as ceil(ctx_len/page) stays as it is; beyond that the next plan takes a new
+ * page off the stack over the table's entry, and the old page is the caller's to push onto the stack first, as are pages that a window has
+ * left behind (whose entries become -1).  A page's scale does not fall when tokens are taken back.
  */
 #ifndef MOE_KV_H
 #define MOE_KV_H
@@ -101,7 +107,8 @@ int32_t moe_kv_plan_within(const moe_kv_step_t *step, const moe_kv_lists_t *list
 
 /* Give back all pages of `n` requests (ids in `requests`, dev; out of range or repeated ones do nothing more), in the order given: their
  * pages go onto the stack, ctx_len[r] becomes 0.  Pages that are no page of the cache, and those that find the
- * stack's `capacity` entries full, are dropped. */
+ * stack's `capacity` entries full, are dropped.  Not between a step's plan and the copying of its kv_len and free_left over ctx_len and
+ * free_count, which would undo it.  Requests are taken one after the other. */
 int32_t moe_kv_release(const int32_t *requests, int32_t n, int32_t n_requests, int32_t n_pages, int32_t page, int32_t max_blocks,
                        int32_t *ctx_len, const int32_t *block_table, int32_t *free_pages, int32_t capacity,
                        int32_t *free_count, void *stream);
@@ -140,7 +147,11 @@ typedef struct {
 } moe_kv_query_t;
 
 /* Attention of a step's rows: out = sum_j softmax(scale * q.k_j) v_j over the cached tokens that the row sees.  A row that sees none gets
- * 0 and lse -inf.  Table entries outside the cache are skipped as if they were masked.  Deterministic: how the work is split follows from the lengths alone. */
+ * 0 and lse -inf.  Table entries outside the cache are skipped as if they were masked.  Deterministic: how the work is split follows from the lengths alone.
+ * Scores, maxima, sums and outputs are held in fp32, codes are exact.  Rounded to fewer bits are: the weights that values are multiplied with, to fp16
+ * (2^-11 of a weight at most; with fp16 outputs the distance from 64 bits is 1.3 times that of fp32 weights, with bf16 outputs the same), and bf16
+ * queries, to fp16 after a power of two is taken off each row (what is 2^38 below a row's largest is dropped).  Both let the matrix units
+ * work on 16-bit operands. */
 int32_t moe_kv_attend(const moe_kv_cache_t *cache, const moe_kv_step_t *step, const void *plan_dev, const int32_t *block_table,
                       const moe_kv_query_t *query, void *scratch, uint64_t scratch_bytes, void *stream);
 

@@ -140,7 +140,8 @@ class Step:
             self.block_table, self._ctx, self._count = block_table, ctx_len, free_count
 
     def advance(self) -> None:
-        """The step is done: its tokens count as cached, its pages as taken."""
+        """The step is done: its tokens count as cached, its pages as taken.  Lengths that are set back afterwards (refused drafts) have to stay
+        within the request's last page: see moe_kv.h."""
         _need(self.block_table is not None, "advance: no plan has been made")
         self._ctx.copy_(self.kv_len)
         self._count.copy_(self.free_left)
@@ -223,7 +224,7 @@ def gather(cache: Cache, slots: torch.Tensor, dtype=torch.float16) -> Tuple[torc
 
 def release(requests: torch.Tensor, n_pages: int, page: int, ctx_len: torch.Tensor, block_table: torch.Tensor, free_pages: torch.Tensor,
             free_count: torch.Tensor) -> None:
-    """Give back the pages of the requests whose ids `requests` holds; their ctx_len becomes 0."""
+    """Give back the pages of the requests whose ids `requests` holds; their ctx_len becomes 0.  Not between a step's plan and its advance."""
     _need(requests.dim() == 1 and block_table.dim() == 2 and free_pages.dim() == 1, "release: requests and free_pages are lists, block_table a table")
     r, m = block_table.shape
     at = _index(block_table)
