@@ -730,8 +730,9 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, const Item &it, 
 // become fp16 numbers once, on their way into LDS: left to the waves, the conversion was a third of their vector instructions, which
 // are the bound here: a prompt of 4096 took 255 us that way, 181 with the codes converted once, parts of prompts 47 and 36.  Places and
 // scales read once for all steps and products of neighbouring steps into different outputs made it 163 to 173 by the machine: 0.80 to 0.84
-// PFLOP/s, 70 % of a large library product.  Matrix unit 35 % of the time, vector unit 43 %, waves waiting 35 % of theirs, no bank conflicts:
-// exponentials, masks and conversions of a step are as many instructions as can be issued beside its products.  The scores of
+// PFLOP/s, 70 % of a large library product.  Matrix unit 35 % of the time, vector unit 43 %, waves waiting 35 % of theirs, no bank conflicts: no
+// unit is full, two waves a SIMD do not cover a step's chain of product, maximum, exponential and product and its barrier.  Both roles' registers
+// come to 256 at D = 128, of which 4 to 5 spill, and 49 to 61 spill at D = 256 (a prompt of 4096: 420 us, floor 237).  The scores of
 // the next step beside the exponentials of this one, orders and priorities asked of the compiler: 0 to 4 % slower.
 template <int D>
 struct ManyShared {

@@ -5,8 +5,8 @@
 // loads wait for its item, then for the block table, then for the scales, 2 to 5 us under load.  So a row's state is kept small, sixteen rows
 // instead of the general kernel's thirty-two (16x16x32 instructions: half the outputs, scores and queries in registers), keys
 // and values are requested anew as soon as they are used, and the next item's way to its tokens goes on under this one's work.
-// D = 128, eight kv heads: one token over 131000 51 us (268 MB, 5.3 TB/s; a plain read of as much 43.7), 64 requests over 500 to 8000
-// 68 (338 MB, 5.0 TB/s; 56.9).  The general kernel takes 53.8 and 73.6 for these, 9.4 instead of 7.4 for one over 700, 65 instead of 35 for one
+// D = 128, eight kv heads: one token over 131000 50 to 52 us by the machine (268 MB, 5.2 TB/s; a plain read of as much 43.7), 64 requests over 500 to 8000
+// 69 (338 MB, 4.9 TB/s; 56.9).  The general kernel takes 53.8 and 73.6 for these, 9.4 instead of 7.4 for one over 700, 65 instead of 35 for one
 // over 60000 with heads of 256.  The roles of lanes and tiles are those of kernels_kv_attend.h with four lane quarters for
 // its two halves: row m of tile t of the scores stands for token 16 (m / 4) + 4 t + m % 4 of a step of 64, so that a lane of
 // quarter g holds the scores of sub-block g in the order in which its sixteen bytes of a value tile hold their codes.
@@ -22,7 +22,7 @@ constexpr int ROWS_DECODE = 16;
 constexpr int DECODE_WAVES = 4;
 
 // Blocks of a compute unit, by their registers.  D = 128, one over 131000 and 64 over 500 to 8000: with one block 47 and 72 us, two 49
-// and 69, three (fewer registers: an item's loads no longer ahead) 67 and 92.  D = 64: with two 29.9 and 42.5, three (whose registers spill) 36.9
+// and 69 (as they then were), three (fewer registers: an item's loads no longer ahead) 67 and 92.  D = 64: with two 29.9 and 42.5, three (whose registers spill) 36.9
 // and 46.2, 512 over 300 39.1 and 50.9; D = 256 has registers for one.
 __host__ __device__ constexpr int decode_blocks(int head_dim) { return head_dim <= 128 ? 2 : 1; }
 

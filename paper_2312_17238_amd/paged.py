@@ -103,7 +103,8 @@ class Cache:
 
 class Step:
     """A step of a ragged batch: its bounds, the lists that `plan` fills (row_start, positions, slots, kv_len, status,
-    free_left) and the workspaces that its layers share.  Made once for bounds that hold for many steps."""
+    free_left) and the workspaces that its layers share.  Made once for bounds that hold for many steps, under the stream that they run on
+    (torch gives its memory to that stream's next tensors when it is dropped).  Threads may share it, streams may not."""
 
     def __init__(self, n_requests: int, n_tokens: int, max_new: int, max_blocks: int, n_pages: int, page: int, q_heads: int, kv_heads: int,
                  head_dim: int, causal: bool = True, window: int = 0, device="cuda:0"):
