@@ -1,6 +1,6 @@
 /*
  * moe_kv.h -- C ABI of the attention half of a decode step on MI355X (gfx950): a paged key/value cache held in
- * 8 bits, the pages of a step's tokens, the store of rotated keys and values, and attention over the cache.
+ * 8 or 4 bits, the pages of a step's tokens, the store of rotated keys and values, and attention over the cache.
  *
  * A step is a ragged batch of requests.  Request r has ctx_len[r] tokens in the cache and brings new_len[r] new ones (one
  * token, a few drafted ones, a prompt or a part of one); the new tokens of all requests are packed row after row,
@@ -11,7 +11,7 @@
  * with other lengths of the same bounds.  The conventions are those of moe_offload.h (status codes, moe_last_error, caller-owned memory and
  * streams); a call is ordered by the stream that it is given and by nothing else.
  *
- * The cache of a layer.  A page holds `page` consecutive tokens of one request.  For every page and kv head there is a
+ * The cache of a layer.  A page holds `page` consecutive tokens of one request.  In 8 bits there is for every page and kv head a
  * run of page * head_dim codes, in tiles of 16 x 16 bytes, and one fp32 scale, for keys and for values each:
  *   k: [n_pages][kv_heads][page/16][head_dim/16][16 tokens][16 dims]
  *   v: [n_pages][kv_heads][page/16][head_dim/16][16 dims][16 tokens]
@@ -20,11 +20,21 @@
  * a single NaN would otherwise reach every token of its page.  A scale is not negative and 2^100 at most; of scales below
  * 2^-96, the store's least, attention takes 2^-96.
  *
+ * In 4 bits (MOE_KV_E2M1) a code stands for 0, 0.5, 1, 1.5, 2, 3, 4 or 6 (0..7) or the negative of that (8..15), and every token has scales of its
+ * own, 2^(byte - 127): one for each 32 dims of a key, one for a value:
+ *   k: [n_pages][kv_heads][page][head_dim/2], a byte two neighbouring dims, the first in its lower half
+ *   k_byte: [n_pages][kv_heads][page/16][4 r][head_dim/32][4 t]: of token 16 s + 4 t + r
+ *   v: [n_pages][kv_heads][page/16][head_dim][8], a byte two neighbouring tokens of a dim, the first in its lower half
+ *   v_byte: [n_pages][kv_heads][page]
+ * Scale bytes are 82 to 172 (2^-45 to 2^45); a cache that is filled by other means than the store keeps to these for the tokens that are cached.
+ * The store clamps numbers to +-65504 (fp16 rows) or +-2^47 (bf16 rows), infinities with them, and takes NaN for 0.  What lies behind a
+ * request's last token may be anything.
+ *
  * Whose pages these are.  A page that gets tokens belongs to one request: two whose tables name the same begun page would both rewrite
  * it.  Full pages that several requests read may be in several tables; before a request is released, its entries of pages that
  * others still read become -1.  Tokens are taken back by lowering ctx_len as long as ceil(ctx_len/page) stays as it is; beyond that the next plan takes a new
  * page off the stack over the table's entry, and the old page is the caller's to push onto the stack first, as are pages that a window has
- * left behind (whose entries become -1).  A page's scale does not fall when tokens are taken back.
+ * left behind (whose entries become -1).  An 8-bit page's scale does not fall when tokens are taken back.
  */
 #ifndef MOE_KV_H
 #define MOE_KV_H
@@ -38,7 +48,8 @@ extern "C" {
 #define MOE_KV_MAX_REQUESTS 4096
 #define MOE_KV_MAX_TOKENS   1048576   /* rows of a step */
 
-enum { MOE_KV_E4M3 = 0, MOE_KV_INT8 = 1 };   /* codes: OCP fp8 e4m3 (largest 448), two's complement (largest 127) */
+enum { MOE_KV_E4M3 = 0, MOE_KV_INT8 = 1,     /* codes: OCP fp8 e4m3 (largest 448), two's complement (largest 127) */
+       MOE_KV_E2M1 = 4 };                    /* ... OCP fp4 e2m1 (largest 6), two in a byte                       */
 enum { MOE_KV_F16 = 0, MOE_KV_BF16 = 1 };    /* 16-bit types of rows                                              */
 
 /* Why a request of a step gets nothing (moe_kv_lists_t.status). */
@@ -54,10 +65,12 @@ typedef struct {
     int32_t page;             /* tokens per page: 16, 32, 64 or 128                                              */
     int32_t kv_heads;         /* 1..256                                                                          */
     int32_t head_dim;         /* 64, 128 or 256                                                                  */
-    int32_t format;           /* MOE_KV_E4M3 or MOE_KV_INT8                                                      */
+    int32_t format;           /* MOE_KV_E4M3, MOE_KV_INT8 or MOE_KV_E2M1                                         */
     int32_t reserved;         /* 0                                                                               */
     void *k, *v;              /* dev, 16-byte aligned                                                            */
-    float *k_scale, *v_scale; /* dev [n_pages][kv_heads]                                                         */
+    union { float *k_scale;   /* dev [n_pages][kv_heads]                                                         */
+            uint8_t *k_byte; };  /* MOE_KV_E2M1: the scales as above, 16-byte aligned                            */
+    union { float *v_scale; uint8_t *v_byte; };
 } moe_kv_cache_t;
 
 /* What the host knows of a step: bounds, not lengths. */
@@ -128,11 +141,13 @@ typedef struct {
     int64_t q_out_stride;
 } moe_kv_rows_t;
 
-/* Norm and rotation of queries and keys in fp32, queries to q_out, keys and values as 8-bit codes to the cache.
- * A page's scale is the smallest power of two, 2^-96 at least, that keeps every number of the page within the format's largest code, and
+/* Norm and rotation of queries and keys in fp32 (keys for a cache in 4 bits in fp64), queries to q_out, keys and values as codes to the cache.
+ * 8 bits: a page's scale is the smallest power of two, 2^-96 at least, that keeps every number of the page within the format's largest code, and
  * at least what it was if tokens of the page are in the cache already.  Where it grows, their codes are rounded again: with a power of two
  * e4m3 codes stay exact but for those that become subnormal, int8 codes move by less than one step of the final scale
- * in all the growths of a page together. */
+ * in all the growths of a page together.
+ * 4 bits: a scale is the smallest power of two, 2^-45 at least, of which six reach every number of the 32 dims (of the value); a code is the nearest,
+ * the even one of two as near.  Nothing that is cached changes when other tokens are stored. */
 int32_t moe_kv_write(const moe_kv_cache_t *cache, const moe_kv_step_t *step, const void *plan_dev, const moe_kv_rows_t *rows,
                      void *stream);
 
@@ -151,7 +166,8 @@ typedef struct {
  * Scores, maxima, sums and outputs are held in fp32, codes are exact.  Rounded to fewer bits are: the weights that values are multiplied with, to fp16
  * (2^-11 of a weight at most; with fp16 outputs the distance from 64 bits is 1.3 times that of fp32 weights, with bf16 outputs the same), and bf16
  * queries, to fp16 after a power of two is taken off each row (what is 2^38 below a row's largest is dropped).  Both let the matrix units
- * work on 16-bit operands. */
+ * work on 16-bit operands.  With a cache in 4 bits the weights are rounded alike, and queries of either type to 21 bits: a number is off by 2^-20 of the
+ * power of two above the largest of its 32 dims (0..31, 32..63, ...) at most, which is nothing for those above 2^-9 of it in fp16 and 2^-12 in bf16. */
 int32_t moe_kv_attend(const moe_kv_cache_t *cache, const moe_kv_step_t *step, const void *plan_dev, const int32_t *block_table,
                       const moe_kv_query_t *query, void *scratch, uint64_t scratch_bytes, void *stream);
 

@@ -30,7 +30,7 @@ EXPORTS = [
 
 # include/moe_kv.h
 MOE_KV_MAX_REQUESTS, MOE_KV_MAX_TOKENS = 4096, 1048576
-MOE_KV_E4M3, MOE_KV_INT8 = 0, 1
+MOE_KV_E4M3, MOE_KV_INT8, MOE_KV_E2M1 = 0, 1, 4
 MOE_KV_F16, MOE_KV_BF16 = 0, 1
 MOE_KV_SERVED, MOE_KV_NO_PAGES, MOE_KV_TOO_LONG, MOE_KV_BAD_SIZE = 0, 1, 2, 3
 KV_EXPORTS = ["moe_kv_plan_bytes", "moe_kv_scratch_bytes", "moe_kv_plan", "moe_kv_plan_within", "moe_kv_release", "moe_kv_write", "moe_kv_attend",

@@ -141,6 +141,46 @@ __device__ __forceinline__ float page_scale(float amax)
     return ldexpf(1.f, e);
 }
 
+// Queries: lds holds (cos, sin) of q_tokens tokens, the first of them t0.
+template <int DTYPE>
+__device__ __forceinline__ void turn_queries(const WriteArgs &a, int t0, uint8_t *lds)
+{
+    const int D = a.c.head_dim, shift = 31 - __builtin_clz(D), L = D / 8, tid = threadIdx.x, rot = a.r.rot_dim, half = rot / 2;
+    const int sub = tid & (L - 1), mine = tid >> (shift - 3), per_pass = WRITE_THREADS >> (shift - 3), d0 = sub * 8;
+    const float per_half = 1.f / (float)half;
+    auto over_half = [&](int i) { return (int)(((float)i + 0.5f) * per_half); };       // i / half
+    const bool rope = rot > 0;
+    float2 *cs = reinterpret_cast<float2 *>(lds);
+    const int n = min(a.q_tokens, a.n_tokens - t0), rows = n * a.q_heads;
+    // lanes past the end repeat the last head, without storing it
+    auto place = [&](int r, int &t, int &h) {
+        r = min(r, rows - 1);
+        t = a.q_tokens == 1 ? 0 : r / a.q_heads;
+        h = r - t * a.q_heads;
+    };
+    int t, h;
+    float x[8], y[8];
+    place(mine, t, h);
+    load8<DTYPE>(a.r.q, (t0 + t) * a.r.q_stride + h * D + d0, a.vec_q, x);
+    if (rope) {
+        for (int i = tid; i < n * half; i += WRITE_THREADS) {
+            const int u = over_half(i);
+            cs[i] = angle(max(a.p.positions[t0 + u], 0), a.r.inv_freq[i - u * half]);
+        }
+        __syncthreads();
+    }
+    for (int r0 = 0; r0 < rows; r0 += per_pass) {
+        const int tt = t, hh = h;
+        place(r0 + per_pass + mine, t, h);
+        load8<DTYPE>(a.r.q, (t0 + t) * a.r.q_stride + h * D + d0, a.vec_q, y);     // the next one's, before this one is stored
+        if (a.r.eps > 0.f) norm8<DTYPE>(x, a.r.eps, a.r.q_gamma, d0, D);
+        if (rope) rotate8(x, cs + tt * half, rot, a.r.interleaved, d0);
+        if (r0 + mine < rows && a.p.positions[t0 + tt] >= 0) store8<DTYPE>(a.r.q_out, (t0 + tt) * a.r.q_out_stride + hh * D + d0, a.vec_qo, x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = y[i];
+    }
+}
+
 template <int DTYPE, int FMT, int ITER>
 __global__ void __launch_bounds__(WRITE_THREADS) k_kv_write(WriteArgs a)
 {
@@ -155,37 +195,7 @@ __global__ void __launch_bounds__(WRITE_THREADS) k_kv_write(WriteArgs a)
     const int block = a.first + blockIdx.x;
 
     if (block >= a.kv_blocks) {
-        // ---- queries: lds holds (cos, sin) of q_tokens tokens
-        float2 *cs = reinterpret_cast<float2 *>(lds);
-        const int t0 = (block - a.kv_blocks) * a.q_tokens;
-        const int n = min(a.q_tokens, a.n_tokens - t0), rows = n * a.q_heads;
-        // lanes past the end repeat the last head, without storing it
-        auto place = [&](int r, int &t, int &h) {
-            r = min(r, rows - 1);
-            t = a.q_tokens == 1 ? 0 : r / a.q_heads;
-            h = r - t * a.q_heads;
-        };
-        int t, h;
-        float x[8], y[8];
-        place(mine, t, h);
-        load8<DTYPE>(a.r.q, (t0 + t) * a.r.q_stride + h * D + d0, a.vec_q, x);
-        if (rope) {
-            for (int i = tid; i < n * half; i += WRITE_THREADS) {
-                const int u = over_half(i);
-                cs[i] = angle(max(a.p.positions[t0 + u], 0), a.r.inv_freq[i - u * half]);
-            }
-            __syncthreads();
-        }
-        for (int r0 = 0; r0 < rows; r0 += per_pass) {
-            const int tt = t, hh = h;
-            place(r0 + per_pass + mine, t, h);
-            load8<DTYPE>(a.r.q, (t0 + t) * a.r.q_stride + h * D + d0, a.vec_q, y);     // the next one's, before this one is stored
-            if (a.r.eps > 0.f) norm8<DTYPE>(x, a.r.eps, a.r.q_gamma, d0, D);
-            if (rope) rotate8(x, cs + tt * half, rot, a.r.interleaved, d0);
-            if (r0 + mine < rows && a.p.positions[t0 + tt] >= 0) store8<DTYPE>(a.r.q_out, (t0 + tt) * a.r.q_out_stride + hh * D + d0, a.vec_qo, x);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = y[i];
-        }
+        turn_queries<DTYPE>(a, (block - a.kv_blocks) * a.q_tokens, lds);
         return;
     }
 

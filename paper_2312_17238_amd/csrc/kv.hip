@@ -1,4 +1,4 @@
-// C ABI of the paged 8-bit key/value cache (see include/moe_kv.h for the contract): argument checks, where a plan's and the
+// C ABI of the paged key/value cache (see include/moe_kv.h for the contract): argument checks, where a plan's and the
 // scratch's parts lie, launches.  Nothing here waits, allocates on the device or keeps state between calls.
 #include <hip/hip_runtime.h>
 
@@ -13,6 +13,8 @@
 #include "kernels_kv_decode.h"
 #include "kernels_kv_plan.h"
 #include "kernels_kv_write.h"
+#include "kernels_kv4_attend.h"
+#include "kernels_kv4_write.h"
 
 using namespace moe;
 using namespace moe::kv;
@@ -52,9 +54,10 @@ static bool step_ok(const moe_kv_step_t *s)
 
 static bool cache_ok(const moe_kv_cache_t *c)
 {
-    return c && geometry_ok(c->n_pages, c->page, c->kv_heads, c->head_dim) && (c->format == MOE_KV_E4M3 || c->format == MOE_KV_INT8) &&
+    const uintptr_t odd = c && c->format == MOE_KV_E2M1 ? 15 : 3;        // scales: whole pieces of sixteen tokens are loaded, or fp32
+    return c && geometry_ok(c->n_pages, c->page, c->kv_heads, c->head_dim) && (c->format == MOE_KV_E4M3 || c->format == MOE_KV_INT8 || c->format == MOE_KV_E2M1) &&
            c->reserved == 0 && c->k && c->v && c->k_scale && c->v_scale && !((uintptr_t)c->k & 15) && !((uintptr_t)c->v & 15) &&
-           !((uintptr_t)c->k_scale & 3) && !((uintptr_t)c->v_scale & 3);
+           !((uintptr_t)c->k_scale & odd) && !((uintptr_t)c->v_scale & odd);
 }
 
 static bool same_geometry(const moe_kv_cache_t *c, const moe_kv_step_t *s)
@@ -215,6 +218,29 @@ static void launch_write(const WriteArgs &a, int iter, dim3 grid, size_t lds, hi
     }
 }
 
+// Into a cache held in 4 bits.
+static int32_t write4(const WriteArgs &args, const Sizes &z, bool turn, hipStream_t s)
+{
+    Write4Args b{};
+    b.w = args;
+    WriteArgs &a = b.w;
+    const int heads = a.c.kv_heads, most = std::min(a.c.page, z.new_most), tokens = std::min(most, SUB), angles = a.r.rot_dim / 2;
+    b.subs = std::min(a.c.page / SUB, (most + 2 * SUB - 2) / SUB);
+    a.heads = std::max(1, std::min(std::min(heads, WRITE_HEADS), WRITE4_ROWS / tokens));
+    b.groups = div_up(heads, a.heads);
+    // below 2^31: 2^17 pieces of at most 2^20 tokens and 4096 requests, 64 groups of heads
+    a.kv_blocks = z.p.max_segments * b.subs * b.groups * 2;
+    a.q_tokens = a.n_tokens >= 2048 ? 2 : 1;
+    const int64_t blocks = (int64_t)a.kv_blocks + (turn ? div_up(a.n_tokens, a.q_tokens) : 0);
+    const size_t lds = std::max<size_t>({(size_t)tokens * angles * sizeof(double2), (size_t)tokens * a.heads * (a.c.head_dim / 2 + 4), (size_t)a.q_tokens * angles * sizeof(float2)});
+    in_pieces(blocks, [&](uint32_t first, unsigned n) {
+        a.first = (int32_t)first;
+        if (a.r.dtype == MOE_KV_F16) hipLaunchKernelGGL((k_kv4_write<MOE_KV_F16>), dim3(n), dim3(WRITE_THREADS), lds, s, b);
+        else hipLaunchKernelGGL((k_kv4_write<MOE_KV_BF16>), dim3(n), dim3(WRITE_THREADS), lds, s, b);
+    });
+    return launched("moe_kv_write");
+}
+
 extern "C" int32_t moe_kv_write(const moe_kv_cache_t *cache, const moe_kv_step_t *step, const void *plan_dev, const moe_kv_rows_t *rows, void *stream)
 {
     if (!cache_ok(cache)) return bad("moe_kv_write: bad or unsupported cache");
@@ -239,6 +265,13 @@ extern "C" int32_t moe_kv_write(const moe_kv_cache_t *cache, const moe_kv_step_t
     a.p = plan_at(z, step->kv_heads, plan_dev);
     a.q_heads = step->q_heads;
     a.n_tokens = step->n_tokens;
+    a.vec_q = rows16(r.q, r.q_stride);
+    a.vec_k = rows16(r.k, r.k_stride);
+    a.vec_v = rows16(r.v, r.v_stride);
+    a.vec_qo = rows16(r.q_out, r.q_out_stride);
+    // queries that neither turn nor move need no block
+    const bool turn = r.rot_dim || r.eps > 0.f || r.q != r.q_out;
+    if (cache->format == MOE_KV_E2M1) return write4(a, z, turn, static_cast<hipStream_t>(stream));
     const int per_pass = WRITE_THREADS / (D / 8), angles = r.rot_dim / 2 * 8, most = std::min(cache->page, z.new_most);
     // heads of a block that stores: as many as fill a pass where requests bring few tokens (256 of one token: 9.6 us, a head a block 15.4)
     a.heads = std::max(1, std::min(std::min(cache->kv_heads, WRITE_HEADS), per_pass / most));
@@ -246,12 +279,6 @@ extern "C" int32_t moe_kv_write(const moe_kv_cache_t *cache, const moe_kv_step_t
     a.kv_blocks = z.p.max_segments * div_up(cache->kv_heads, a.heads) * 2;
     // Two tokens of a query block once there are blocks enough: 8 thousand tokens 47.9 us, with four 48.6; one fills more of the GPU before that.
     a.q_tokens = step->n_tokens >= 2048 ? 2 : 1;
-    a.vec_q = rows16(r.q, r.q_stride);
-    a.vec_k = rows16(r.k, r.k_stride);
-    a.vec_v = rows16(r.v, r.v_stride);
-    a.vec_qo = rows16(r.q_out, r.q_out_stride);
-    // queries that neither turn nor move need no block
-    const bool turn = r.rot_dim || r.eps > 0.f || r.q != r.q_out;
     const int64_t blocks = (int64_t)z.p.max_segments * div_up(cache->kv_heads, a.heads) * 2 + (turn ? div_up(step->n_tokens, a.q_tokens) : 0);
     const size_t lds = std::max<size_t>((size_t)a.lds_rows * (D + 16) + per_pass * angles, (size_t)a.q_tokens * angles);
     int iter = 1;
@@ -285,6 +312,16 @@ static void launch_attend(const AttendArgs &a, int D, bool decode, dim3 grid, hi
     case 64: hipLaunchKernelGGL((k_kv_attend<DTYPE, FMT, 64>), grid, dim3(64 * ATTEND_WAVES), 0, s, a); break;
     case 128: hipLaunchKernelGGL((k_kv_attend<DTYPE, FMT, 128>), grid, dim3(64 * ATTEND_WAVES), 0, s, a); break;
     default: hipLaunchKernelGGL((k_kv_attend<DTYPE, FMT, 256>), grid, dim3(64 * ATTEND_WAVES), 0, s, a); break;
+    }
+}
+
+template <int DTYPE>
+static void launch_attend4(const AttendArgs &a, int D, dim3 grid, hipStream_t s)
+{
+    switch (D) {
+    case 64: hipLaunchKernelGGL((k_kv4_attend<DTYPE, 64>), grid, dim3(64 * ATTEND_WAVES), 0, s, a); break;
+    case 128: hipLaunchKernelGGL((k_kv4_attend<DTYPE, 128>), grid, dim3(64 * ATTEND_WAVES), 0, s, a); break;
+    default: hipLaunchKernelGGL((k_kv4_attend<DTYPE, 256>), grid, dim3(64 * ATTEND_WAVES), 0, s, a); break;
     }
 }
 
@@ -327,7 +364,10 @@ extern "C" int32_t moe_kv_attend(const moe_kv_cache_t *cache, const moe_kv_step_
     a.many_blocks = (int32_t)many;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const dim3 grid((unsigned)blocks);
-    if (q.dtype == MOE_KV_F16) {
+    if (cache->format == MOE_KV_E2M1) {
+        if (q.dtype == MOE_KV_F16) launch_attend4<MOE_KV_F16>(a, D, grid, s);
+        else launch_attend4<MOE_KV_BF16>(a, D, grid, s);
+    } else if (q.dtype == MOE_KV_F16) {
         if (cache->format == MOE_KV_E4M3) launch_attend<MOE_KV_F16, MOE_KV_E4M3>(a, D, z.decode, grid, s);
         else launch_attend<MOE_KV_F16, MOE_KV_INT8>(a, D, z.decode, grid, s);
     } else {
@@ -346,7 +386,10 @@ extern "C" int32_t moe_kv_gather(const moe_kv_cache_t *cache, const int32_t *slo
     const hipStream_t s = static_cast<hipStream_t>(stream);
     in_pieces((int64_t)div_up(n, SUB) * cache->kv_heads, [&](uint32_t first, unsigned blocks) {
         const dim3 grid(blocks);
-        if (dtype == MOE_KV_F16) {
+        if (cache->format == MOE_KV_E2M1) {
+            if (dtype == MOE_KV_F16) hipLaunchKernelGGL((k_kv4_gather<MOE_KV_F16>), grid, dim3(256), 0, s, *cache, first, slots, n, k_out, v_out);
+            else hipLaunchKernelGGL((k_kv4_gather<MOE_KV_BF16>), grid, dim3(256), 0, s, *cache, first, slots, n, k_out, v_out);
+        } else if (dtype == MOE_KV_F16) {
             if (cache->format == MOE_KV_E4M3) hipLaunchKernelGGL((k_kv_gather<MOE_KV_F16, MOE_KV_E4M3>), grid, dim3(256), 0, s, *cache, first, slots, n, k_out, v_out);
             else hipLaunchKernelGGL((k_kv_gather<MOE_KV_F16, MOE_KV_INT8>), grid, dim3(256), 0, s, *cache, first, slots, n, k_out, v_out);
         } else {

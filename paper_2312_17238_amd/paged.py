@@ -1,4 +1,4 @@
-"""Tensors around include/moe_kv.h: a paged 8-bit key/value cache and the attention half of a decode step.
+"""Tensors around include/moe_kv.h: a paged key/value cache in 8 or 4 bits and the attention half of a decode step.
 
     cache = Cache.empty(n_pages, kv_heads, head_dim)                    # one per layer
     step = Step(n_requests, n_tokens, max_new, max_blocks, n_pages, page, q_heads, kv_heads, head_dim)
@@ -22,7 +22,7 @@ import torch
 from . import binding as B
 
 DTYPES = {torch.float16: B.MOE_KV_F16, torch.bfloat16: B.MOE_KV_BF16}
-FORMATS = {torch.float8_e4m3fn: B.MOE_KV_E4M3, torch.int8: B.MOE_KV_INT8}
+FORMATS = {torch.float8_e4m3fn: B.MOE_KV_E4M3, torch.int8: B.MOE_KV_INT8, torch.float4_e2m1fn_x2: B.MOE_KV_E2M1}
 
 # A call costs the host a few microseconds, which for single tokens is what counts: structures and references to them are made once,
 # messages only when something is refused.
@@ -72,22 +72,33 @@ def _rows(t: torch.Tensor, shape, dtype, device: int, what: str) -> Tuple[int, i
 
 
 class Cache:
-    """Keys and values of one layer: 8-bit codes in 16 x 16 tiles and a scale for each page and kv head.
+    """Keys and values of one layer: codes in the order that the attention reads them in, and their scales.
 
-    k: [n_pages, kv_heads, page/16, head_dim/16, 16 tokens, 16 dims], v: [n_pages, kv_heads, page/16, head_dim, 16 tokens]
-    (float8_e4m3fn or int8); k_scale, v_scale: [n_pages, kv_heads] fp32."""
+    float8_e4m3fn or int8: k [n_pages, kv_heads, page/16, head_dim/16, 16 tokens, 16 dims], v [n_pages, kv_heads, page/16, head_dim, 16 tokens];
+    k_scale, v_scale [n_pages, kv_heads] fp32, one for each page and kv head.
+    float4_e2m1fn_x2, two codes in a byte: k [n_pages, kv_heads, page, head_dim/2], v [n_pages, kv_heads, page/16, head_dim, 8]; float8_e8m0fnu
+    scales, a key's for each 32 dims k_scale [n_pages, kv_heads, page/16, 4 r, head_dim/32, 4 t] (token 16 s + 4 t + r), a value's
+    v_scale [n_pages, kv_heads, page]."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
-        _need(k.dim() == 6 and k.shape[4:] == (16, 16), f"Cache: k has shape {tuple(k.shape)}")
-        p, h, s, d = k.shape[:4]
-        _need(tuple(v.shape) == (p, h, s, 16 * d, 16), f"Cache: v has shape {tuple(v.shape)}")
         _need(k.dtype in FORMATS and v.dtype == k.dtype, f"Cache: codes of type {k.dtype} and {v.dtype}")
-        for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
-            _need(tuple(t.shape) == (p, h) and t.dtype == torch.float32, f"Cache: {what} is {t.dtype} {tuple(t.shape)}")
+        four = k.dtype is torch.float4_e2m1fn_x2
+        if four:
+            _need(k.dim() == 4, f"Cache: k has shape {tuple(k.shape)}")
+            p, h, page, d = k.shape[0], k.shape[1], k.shape[2], 2 * k.shape[3]
+            scales, kind = ((p, h, page // 16, 4, d // 32, 4), (p, h, page)), torch.float8_e8m0fnu
+            _need(tuple(v.shape) == (p, h, page // 16, d, 8), f"Cache: v has shape {tuple(v.shape)}")
+        else:
+            _need(k.dim() == 6 and k.shape[4:] == (16, 16), f"Cache: k has shape {tuple(k.shape)}")
+            p, h, page, d = k.shape[0], k.shape[1], 16 * k.shape[2], 16 * k.shape[3]
+            scales, kind = ((p, h), (p, h)), torch.float32
+            _need(tuple(v.shape) == (p, h, page // 16, d, 16), f"Cache: v has shape {tuple(v.shape)}")
+        for t, shape, what in ((k_scale, scales[0], "k_scale"), (v_scale, scales[1], "v_scale")):
+            _need(tuple(t.shape) == shape and t.dtype == kind, f"Cache: {what} is {t.dtype} {tuple(t.shape)}, {kind} {shape} is needed")
         _need(all(t.is_cuda and t.is_contiguous() and t.device == k.device for t in (k, v, k_scale, v_scale)), "Cache: contiguous tensors on one GPU are needed")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.n_pages, self.kv_heads, self.page, self.head_dim = p, h, 16 * s, 16 * d
-        self.c = B.KvCache(p, 16 * s, h, 16 * d, FORMATS[k.dtype], 0, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+        self.n_pages, self.kv_heads, self.page, self.head_dim = p, h, page, d
+        self.c = B.KvCache(p, page, h, d, FORMATS[k.dtype], 0, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
         self.ref = C.byref(self.c)
         self.device = _index(k)
 
@@ -95,8 +106,14 @@ class Cache:
     def empty(cls, n_pages: int, kv_heads: int, head_dim: int, page: int = 64, dtype=torch.float8_e4m3fn, device="cuda:0") -> "Cache":
         """Uninitialised: a page's content counts from the first token that is written into it."""
         _need(page % 16 == 0 and head_dim % 16 == 0, "Cache: page and head_dim have to be multiples of 16")
-        k = torch.empty(n_pages, kv_heads, page // 16, head_dim // 16, 16, 16, dtype=torch.uint8, device=device)
-        v = torch.empty(n_pages, kv_heads, page // 16, head_dim, 16, dtype=torch.uint8, device=device)
+        b = lambda *shape: torch.empty(*shape, dtype=torch.uint8, device=device)  # noqa: E731
+        if dtype is torch.float4_e2m1fn_x2:
+            _need(head_dim % 32 == 0, "Cache: head_dim has to be a multiple of 32")
+            scale = torch.float8_e8m0fnu
+            return cls(b(n_pages, kv_heads, page, head_dim // 2).view(dtype), b(n_pages, kv_heads, page // 16, head_dim, 8).view(dtype),
+                       b(n_pages, kv_heads, page // 16, 4, head_dim // 32, 4).view(scale), b(n_pages, kv_heads, page).view(scale))
+        k = b(n_pages, kv_heads, page // 16, head_dim // 16, 16, 16)
+        v = b(n_pages, kv_heads, page // 16, head_dim, 16)
         s = torch.empty(2, n_pages, kv_heads, dtype=torch.float32, device=device)
         return cls(k.view(dtype), v.view(dtype), s[0], s[1])
 
