@@ -22,6 +22,7 @@ namespace kv {
 
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef unsigned int v6u __attribute__((ext_vector_type(6)));
+typedef float v32f __attribute__((ext_vector_type(32)));
 
 constexpr int DIGITS = 4;
 
@@ -51,18 +52,22 @@ __device__ __forceinline__ Digits digits_of(float (&x)[32], uint32_t top, int ro
     Digits r;
     const int e = max((int)(top >> 23), 1);
 #pragma unroll
-    for (int j = 0; j < 32; ++j) x[j] = ldexpf(x[j], 130 - e);      // eighths: below 16 in size
+    for (int j = 0; j < 32; ++j) x[j] = ldexpf(x[j], 127 - e);      // below 2 in size
 #pragma unroll
     for (int p = 0; p < DIGITS; ++p) {
         v16f even, odd;
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            const float n = rintf(x[j]);
-            if (j % 2) odd[j / 2] = n;
-            else even[j / 2] = n;
-            x[j] = (x[j] - n) * 32.f;
+        for (int j = 0; j < 16; ++j) {
+            even[j] = x[2 * j];
+            odd[j] = x[2 * j + 1];
         }
-        r.d[p] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, 8.f);
+        // to the nearest eighth, and what is left of it times 32: 2 at most
+        r.d[p] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, 1.f);
+        if (p + 1 < DIGITS) {
+            const v32f n = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(r.d[p], 32.f);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) x[j] = fmaf(x[j], 32.f, -n[j]);
+        }
     }
     const int b = 127 + 14 + max(e - row, -100);
     r.scale = b | (b - 5) << 8 | (b - 10) << 16 | (b - 15) << 24;

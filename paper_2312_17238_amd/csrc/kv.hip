@@ -14,6 +14,7 @@
 #include "kernels_kv_plan.h"
 #include "kernels_kv_write.h"
 #include "kernels_kv4_attend.h"
+#include "kernels_kv4_decode.h"
 #include "kernels_kv4_write.h"
 
 using namespace moe;
@@ -316,8 +317,16 @@ static void launch_attend(const AttendArgs &a, int D, bool decode, dim3 grid, hi
 }
 
 template <int DTYPE>
-static void launch_attend4(const AttendArgs &a, int D, dim3 grid, hipStream_t s)
+static void launch_attend4(const AttendArgs &a, int D, bool decode, dim3 grid, hipStream_t s)
 {
+    if (decode) {
+        switch (D) {
+        case 64: hipLaunchKernelGGL((k_kv4_decode<DTYPE, 64>), grid, dim3(64 * DECODE_WAVES), 0, s, a); break;
+        case 128: hipLaunchKernelGGL((k_kv4_decode<DTYPE, 128>), grid, dim3(64 * DECODE_WAVES), 0, s, a); break;
+        default: hipLaunchKernelGGL((k_kv4_decode<DTYPE, 256>), grid, dim3(64 * DECODE_WAVES), 0, s, a); break;
+        }
+        return;
+    }
     switch (D) {
     case 64: hipLaunchKernelGGL((k_kv4_attend<DTYPE, 64>), grid, dim3(64 * ATTEND_WAVES), 0, s, a); break;
     case 128: hipLaunchKernelGGL((k_kv4_attend<DTYPE, 128>), grid, dim3(64 * ATTEND_WAVES), 0, s, a); break;
@@ -365,8 +374,8 @@ extern "C" int32_t moe_kv_attend(const moe_kv_cache_t *cache, const moe_kv_step_
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const dim3 grid((unsigned)blocks);
     if (cache->format == MOE_KV_E2M1) {
-        if (q.dtype == MOE_KV_F16) launch_attend4<MOE_KV_F16>(a, D, grid, s);
-        else launch_attend4<MOE_KV_BF16>(a, D, grid, s);
+        if (q.dtype == MOE_KV_F16) launch_attend4<MOE_KV_F16>(a, D, z.decode, grid, s);
+        else launch_attend4<MOE_KV_BF16>(a, D, z.decode, grid, s);
     } else if (q.dtype == MOE_KV_F16) {
         if (cache->format == MOE_KV_E4M3) launch_attend<MOE_KV_F16, MOE_KV_E4M3>(a, D, z.decode, grid, s);
         else launch_attend<MOE_KV_F16, MOE_KV_INT8>(a, D, z.decode, grid, s);
