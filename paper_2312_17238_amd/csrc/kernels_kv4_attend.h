@@ -354,7 +354,7 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, const Item &it,
             }
         }
     }
-    if (!whole && all_parts_done(a.p.joins_few + it.join * heads + head, it.parts, sh.join)) join_parts<DTYPE, D>(a, it, head, a.part_few, ml, ROWS_FEW, sh.join);
+    if (!whole && all_parts_done(a.p.joins_few + it.join * heads + head, it.parts, sh.join.last)) join_parts<DTYPE, D>(a, it, head, a.part_few, ml, ROWS_FEW, sh.join);
 }
 
 // ---- tiles of 32 rows a wave: every wave has its own and takes all steps of the block's.
@@ -395,7 +395,7 @@ __device__ __forceinline__ void attend4_many(const AttendArgs &a, const Item &it
             else if (a.q.lse) a.q.lse[(int64_t)(it.row0 + row.tok) * heads * a.group + head * a.group + row.g] = s.l == 0.f ? -INFINITY : LN2 * (s.m + log2f(s.l));
         }
     }
-    if (!whole && all_parts_done(a.p.joins_many + it.join * heads + head, it.parts, sh)) join_tile<DTYPE, D, ROWS>(a, it, head, parts, ml, sh);
+    if (!whole && all_parts_done(a.p.joins_many + it.join * heads + head, it.parts, sh.last)) join_tile<DTYPE, D, ROWS>(a, it, head, parts, ml, sh);
 }
 
 template <int DTYPE, int D>

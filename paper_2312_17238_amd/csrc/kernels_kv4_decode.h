@@ -12,6 +12,98 @@
 namespace moe {
 namespace kv {
 
+// Joining the parts of a tile's rows, in the parts' order.  What this costs is not its bytes but one wait behind the other, those for code that is not in
+// the instruction cache among them: one short loop without a branch inside, which takes a part's maximum, sum and outputs in one go.
+struct Join4Shared {
+    float4 sum[64 * DECODE_WAVES];      // of a thread
+    float2 ml[64 * DECODE_WAVES];
+    int last;
+};
+
+template <int DTYPE, int D>
+__device__ __forceinline__ void join4(const AttendArgs &a, const Item &it, int head, const float *ml, Join4Shared &sh)
+{
+    constexpr int THREADS = 64 * DECODE_WAVES, QUADS = D / 4, SPAN = 16;
+    const int tid = threadIdx.x, heads = a.c.kv_heads, rows = it.n_new * a.group, parts = it.parts;
+    int pow2 = 4;
+    while (pow2 < rows) pow2 *= 2;
+    const __amdgpu_buffer_rsrc_t o = __builtin_amdgcn_make_buffer_rsrc(a.part_few, 0, (int)((uint32_t)(a.p.parts_few * heads * ROWS_FEW) * (D * 4u)), 0x00020000);
+    // four dims a thread; where that leaves threads over, the parts are dealt out to groups of waves
+    const int all = min(THREADS, pow2 * QUADS), groups = THREADS / all, g = __builtin_amdgcn_readfirstlane(tid / all);
+    // 32 bits: at most 1024 parts of all heads, of 32 rows and 256 dims
+    const uint32_t first = (uint32_t)(it.part0 * heads + head) * ROWS_FEW, stride = (uint32_t)heads * ROWS_FEW;
+#pragma nounroll
+    for (int e = tid % all; e < pow2 * QUADS; e += all) {
+        const int r = min(e / QUADS, rows - 1), d = (e % QUADS) * 4;
+        float top = -INFINITY, l = 0.f;
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma nounroll
+        for (int p0 = g; p0 < parts; p0 += SPAN * groups) {
+            float4 x[SPAN];
+            float2 v[SPAN];
+            float high = top;
+#pragma unroll
+            for (int u = 0; u < SPAN; ++u) {            // past the last part that one again, which then does not count
+                const uint32_t at = first + (uint32_t)min(p0 + u * groups, parts - 1) * stride;
+                v[u] = get2(ml, (at + r) * 8);
+                x[u] = __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(o, (r * D + d) * 4, (int)(at * (D * 4)), 16));
+            }
+#pragma unroll
+            for (int u = 0; u < SPAN; ++u) high = fmaxf(high, v[u].x);
+            const float base = high == -INFINITY ? 0.f : high, f = exp2f(top - base);
+            top = high;
+            l *= f;
+            sum.x *= f;
+            sum.y *= f;
+            sum.z *= f;
+            sum.w *= f;
+#pragma unroll
+            for (int u = 0; u < SPAN; ++u) {
+                const float w = p0 + u * groups < parts ? exp2f(v[u].x - base) : 0.f;
+                l = fmaf(w, v[u].y, l);
+                sum.x = fmaf(w, x[u].x, sum.x);
+                sum.y = fmaf(w, x[u].y, sum.y);
+                sum.z = fmaf(w, x[u].z, sum.z);
+                sum.w = fmaf(w, x[u].w, sum.w);
+            }
+        }
+        if (groups > 1) {
+            sh.sum[tid] = sum;
+            sh.ml[tid] = make_float2(top, l);
+            __syncthreads();
+            float high = top;
+            for (int w = 1; w < groups; ++w) high = fmaxf(high, sh.ml[w * all + e].x);
+            const float base = high == -INFINITY ? 0.f : high;
+            l = 0.f;
+            sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int w = 0; w < groups; ++w) {
+                const float2 v = sh.ml[w * all + e];
+                const float4 x = sh.sum[w * all + e];
+                const float f = exp2f(v.x - base);
+                l = fmaf(f, v.y, l);
+                sum.x = fmaf(f, x.x, sum.x);
+                sum.y = fmaf(f, x.y, sum.y);
+                sum.z = fmaf(f, x.z, sum.z);
+                sum.w = fmaf(f, x.w, sum.w);
+            }
+            top = high;
+        }
+        if (g == 0 && e < rows * QUADS) {
+            const float f = l == 0.f ? 0.f : 1.f / l;
+            const int tok = r / a.group, gr = r - tok * a.group;
+            store4<DTYPE>(a.q.out, (it.row0 + tok) * a.q.out_stride + (int64_t)(head * a.group + gr) * D + d, a.vec_out, sum.x * f, sum.y * f, sum.z * f, sum.w * f);
+            if (a.q.lse && d == 0) a.q.lse[(int64_t)(it.row0 + tok) * heads * a.group + head * a.group + gr] = l == 0.f ? -INFINITY : LN2 * (top + log2f(l));
+        }
+    }
+}
+
+template <int D>
+struct Decode4Shared {
+    float m[DECODE_WAVES][ROWS_DECODE], l[DECODE_WAVES][ROWS_DECODE];
+    __align__(16) float o[DECODE_WAVES * 8 * (D + 4)];
+    Join4Shared join;
+};
+
 // What is known of an item before it is worked on: where the sub-blocks of its first sixteen steps lie, which of them are in the cache, queries.
 template <int D>
 struct Ahead4 {
@@ -29,7 +121,7 @@ struct Decode4 {
     struct Values { uint4 v[D / 32], scale; };
 
     const AttendArgs &a;
-    DecodeShared<D> &sh;
+    Decode4Shared<D> &sh;
     const int head, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
 
     __device__ __forceinline__ static int steps(const Item &it) { return div_up(it.kt1 - it.kt0, 2); }
@@ -319,14 +411,14 @@ struct Decode4 {
 
     __device__ __forceinline__ void join(const Item &it) const
     {
-        if (all_parts_done(a.p.joins_few + it.join * a.c.kv_heads + head, it.parts, sh.join)) join_parts<DTYPE, D>(a, it, head, a.part_few, ml(), ROWS_FEW, sh.join);
+        if (all_parts_done(a.p.joins_few + it.join * a.c.kv_heads + head, it.parts, sh.join.last)) join4<DTYPE, D>(a, it, head, ml(), sh.join);
     }
 };
 
 template <int DTYPE, int D>
 __global__ void __launch_bounds__(64 * DECODE_WAVES, decode_blocks(D)) k_kv4_decode(AttendArgs a)
 {
-    __shared__ DecodeShared<D> sh;
+    __shared__ Decode4Shared<D> sh;
     const int i = blockIdx.x / a.c.kv_heads;
     const int first = a.p.few_first[i], last = a.p.few_first[i + 1] - 1;
     if (i >= a.p.head->few_blocks) return;
@@ -357,8 +449,12 @@ __global__ void __launch_bounds__(64 * DECODE_WAVES, decode_blocks(D)) k_kv4_dec
         after.id = d.table(next, d.wave);
         __syncthreads();          // the item before is done with LDS
     }
-    if (first != last && split.part >= 0) d.join(split);
-    if (it.part >= 0) d.join(it);
+#pragma nounroll
+    for (int u = first != last ? 0 : 1; u < 2; ++u) {
+        const Item joined = u ? it : split;
+        if (joined.part >= 0) d.join(joined);
+        __syncthreads();          // done with LDS
+    }
 }
 
 }  // namespace kv

@@ -414,16 +414,16 @@ struct JoinShared {
 };
 
 // Counts this block's part; true in the block that came last.  Every thread's stores are acknowledged before the count.
-__device__ __forceinline__ bool all_parts_done(int32_t *count, int parts, JoinShared &sh)
+__device__ __forceinline__ bool all_parts_done(int32_t *count, int parts, int &last)
 {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if (threadIdx.x == 0) {
-        sh.last = __hip_atomic_fetch_add(count, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
-        if (sh.last) __hip_atomic_store(count, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);     // for the next layer
+        last = __hip_atomic_fetch_add(count, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
+        if (last) __hip_atomic_store(count, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);     // for the next layer
     }
     __syncthreads();
-    return sh.last;
+    return last;
 }
 
 // (m, l) of two parts of a row.
@@ -723,7 +723,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs &a, const Item &it, 
             }
         }
     }
-    if (!whole && all_parts_done(a.p.joins_few + it.join * heads + head, it.parts, sh.join)) join_parts<DTYPE, D>(a, it, head, a.part_few, ml, ROWS_FEW, sh.join);
+    if (!whole && all_parts_done(a.p.joins_few + it.join * heads + head, it.parts, sh.join.last)) join_parts<DTYPE, D>(a, it, head, a.part_few, ml, ROWS_FEW, sh.join);
 }
 
 // ---- tiles of 32 rows a wave: every wave has its own, all waves share the block's steps through LDS, two at a time.  The codes
@@ -862,7 +862,7 @@ __device__ __forceinline__ void attend_many(const AttendArgs &a, const Item &it,
             else if (a.q.lse) a.q.lse[(int64_t)(it.row0 + tok) * heads * a.group + head * a.group + g] = s.l == 0.f ? -INFINITY : LN2 * (s.m + log2f(s.l));
         }
     }
-    if (!whole && all_parts_done(a.p.joins_many + it.join * heads + head, it.parts, sh.join)) join_tile<DTYPE, D, ROWS>(a, it, head, parts, ml, sh.join);
+    if (!whole && all_parts_done(a.p.joins_many + it.join * heads + head, it.parts, sh.join.last)) join_tile<DTYPE, D, ROWS>(a, it, head, parts, ml, sh.join);
 }
 
 template <int DTYPE, int FMT, int D>

@@ -328,7 +328,7 @@ struct Decode {
 
     __device__ __forceinline__ void join(const Item &it) const
     {
-        if (all_parts_done(a.p.joins_few + it.join * a.c.kv_heads + head, it.parts, sh.join)) join_parts<DTYPE, D>(a, it, head, a.part_few, ml(), ROWS_FEW, sh.join);
+        if (all_parts_done(a.p.joins_few + it.join * a.c.kv_heads + head, it.parts, sh.join.last)) join_parts<DTYPE, D>(a, it, head, a.part_few, ml(), ROWS_FEW, sh.join);
     }
 };
 
