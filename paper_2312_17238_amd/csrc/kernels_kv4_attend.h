@@ -182,6 +182,7 @@ __device__ __forceinline__ void step4(State4<D> &s, const Rows4<D> &r, const uin
 #pragma unroll
     for (int i = 0; i < 16; ++i) z[i] = fmaf(z[i], r.factor, byte_of(b[i / 4], i % 4));
     if (edge) {
+        asm volatile("");               // a branch: as selections this would be worked out for every step
 #pragma unroll
         for (int i = 0; i < 16; ++i) z[i] = i >= see.lo && i < see.hi ? z[i] : -INFINITY;
     }

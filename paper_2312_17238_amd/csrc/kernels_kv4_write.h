@@ -20,6 +20,7 @@ struct Write4Args {
     WriteArgs w;            // heads: of a block that stores; kv_blocks: blocks that store
     int32_t subs;           // pieces of sixteen that a segment's tokens can lie in
     int32_t groups;         // blocks that share a piece's heads
+    uint32_t blocks;        // of the whole grid, fewer than 2^32
 };
 
 // Cosine and sine of pos * freq in fp64.  The product is exact (24 bits each).  The nearest quarter turn is taken off with pi/2 in two parts; the
@@ -116,11 +117,13 @@ __global__ void __launch_bounds__(WRITE_THREADS) k_kv4_write(Write4Args b)
     const int D = a.c.head_dim, shift = 31 - __builtin_clz(D), L = D / 8, tid = threadIdx.x, rot = a.r.rot_dim, half = rot / 2;
     const int sub = tid & (L - 1), mine = tid >> (shift - 3), per_pass = WRITE_THREADS >> (shift - 3), d0 = sub * 8;
     extern __shared__ __align__(16) uint8_t write4_lds[];
-    const int block = a.first + blockIdx.x;
-    if (block >= a.kv_blocks) {
-        turn_queries<DTYPE>(a, (block - a.kv_blocks) * a.q_tokens, write4_lds);
+    // blocks that store are spread evenly among those of queries: these wait for memory, those for their fp64 sums
+    const uint32_t index = a.first + blockIdx.x, before = (uint32_t)((uint64_t)index * a.kv_blocks / b.blocks), through = (uint32_t)((uint64_t)(index + 1) * a.kv_blocks / b.blocks);
+    if (through == before) {
+        turn_queries<DTYPE>(a, (int)(index - before) * a.q_tokens, write4_lds);
         return;
     }
+    const int block = (int)before;
     const int which = block & 1, unit = (block >> 1) / b.groups, h0 = ((block >> 1) - unit * b.groups) * a.heads, si = unit / b.subs;
     const int heads = a.c.kv_heads, page = a.c.page, hg = min(a.heads, heads - h0);
     const Segment s = a.p.segments[si];         // in flight with the list's length
@@ -146,22 +149,23 @@ __global__ void __launch_bounds__(WRITE_THREADS) k_kv4_write(Write4Args b)
     uint4 next = fetch(mine);
 
     if (!which) {
+        // a token's angles: 8 j + i at [i][j], so that neighbouring threads, eight dims each, find theirs side by side
         double2 *cs = reinterpret_cast<double2 *>(write4_lds);
+        const int eighth = half / 8;
         const float per_half = 1.f / (float)half;
         for (int i = tid; i < n * half; i += WRITE_THREADS) {
-            const int u = (int)(((float)i + 0.5f) * per_half);
-            cs[i] = angle64(pos0 + u, a.r.inv_freq[i - u * half]);
+            const int u = (int)(((float)i + 0.5f) * per_half), k = i - u * half;
+            cs[u * half + (k & 7) * eighth + (k >> 3)] = angle64(pos0 + u, a.r.inv_freq[k]);
         }
         if (half) __syncthreads();
         // a dim's partner in its pair: itself's neighbour, or half of the rotated dims away
         const bool turns = d0 < rot, second = d0 >= half;
         const int away = a.r.interleaved || !turns ? 0 : second ? -half / 8 : half / 8, from = (tid & 63) + away, p0 = d0 + 8 * away;
-        float g[8], pg[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) g[i] = pg[i] = 1.f;
+        const uint32_t one = to_bits<DTYPE>(1.f) * 0x10001u;
+        uint4 gain = make_uint4(one, one, one, one), pgain = gain;      // of the dims and of their partners
         if (a.r.eps > 0.f && a.r.k_gamma) {
-            load8<DTYPE>(a.r.k_gamma, d0, false, g);
-            load8<DTYPE>(a.r.k_gamma, p0, false, pg);
+            gain = load_raw8<DTYPE>(a.r.k_gamma, d0, false);
+            pgain = load_raw8<DTYPE>(a.r.k_gamma, p0, false);
         }
         for (int r0 = 0; r0 < rows; r0 += per_pass) {
             const uint4 raw = next;
@@ -182,10 +186,13 @@ __global__ void __launch_bounds__(WRITE_THREADS) k_kv4_write(Write4Args b)
                 if (rot && !a.r.interleaved)
                     floats_of<DTYPE>(make_uint4(__shfl((int)raw.x, from), __shfl((int)raw.y, from), __shfl((int)raw.z, from), __shfl((int)raw.w, from)), y);
                 const double2 *at = cs + t * half;
+                float g[8], pg[8];
+                floats_of<DTYPE>(gain, g);
+                floats_of<DTYPE>(pgain, pg);
                 if (turns && a.r.interleaved) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const double2 w = at[d0 / 2 + i];
+                        const double2 w = at[((sub & 1) * 4 + i) * eighth + (sub >> 1)];
                         const double u = (double)x[2 * i] * f * g[2 * i], v = (double)x[2 * i + 1] * f * g[2 * i + 1];
                         x[2 * i] = to_odd(u * w.x - v * w.y);
                         x[2 * i + 1] = to_odd(u * w.y + v * w.x);
@@ -193,7 +200,7 @@ __global__ void __launch_bounds__(WRITE_THREADS) k_kv4_write(Write4Args b)
                 } else if (turns) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const double2 w = at[(second ? d0 - half : d0) + i];
+                        const double2 w = at[i * eighth + (second ? sub - eighth : sub)];
                         const double u = (double)x[i] * f * g[i], v = (double)y[i] * f * pg[i];
                         x[i] = to_odd(second ? v * w.y + u * w.x : u * w.x - v * w.y);
                     }
@@ -255,63 +262,65 @@ __global__ void __launch_bounds__(WRITE_THREADS) k_kv4_write(Write4Args b)
     }
 }
 
-// Sixteen entries of the list and one head.  Two waves take the keys, 32 dims of a token a thread; two the values, two dims of all sixteen
-// tokens a thread, whose pieces of sixteen tokens are loaded anew only where the next entry lies in another one.
+// Sixteen entries of the list and one head.  A thread takes eight dims: of an entry's key (four bytes in, sixteen out), and of the values of
+// as many entries as the block has turns left, whose pieces of sixteen tokens it loads anew only where the next entry lies in another one.
+template <int DTYPE>
+__device__ __forceinline__ uint4 e2m1_to_16bit(uint32_t w, float s)
+{
+    const auto p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0), q = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1);
+    const auto r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 2), t = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 3);
+    return make_uint4(pack2<DTYPE>(p[0], p[1]), pack2<DTYPE>(q[0], q[1]), pack2<DTYPE>(r[0], r[1]), pack2<DTYPE>(t[0], t[1]));
+}
+
 template <int DTYPE>
 __global__ void __launch_bounds__(256) k_kv4_gather(moe_kv_cache_t c, uint32_t first, const int32_t *slots, int n, void *k_out, void *v_out)
 {
-    const int D = c.head_dim, page_shift = 31 - __builtin_clz(c.page), page = c.page, heads = c.kv_heads;
+    const int D = c.head_dim, shift = 31 - __builtin_clz(D), L = D / 8, page_shift = 31 - __builtin_clz(c.page), page = c.page, heads = c.kv_heads;
     const uint32_t block = first + blockIdx.x;      // of the whole grid
-    const int head = block % heads, e0 = (block / heads) * SUB, tid = threadIdx.x & 127;
+    const int head = block % heads, e0 = (block / heads) * SUB, tid = threadIdx.x & 127, sub = tid & (L - 1), mine = tid >> (shift - 3), at_once = 128 >> (shift - 3);
     const int m = min(SUB, n - e0);
     const uint32_t limit = (uint32_t)c.n_pages * page;
-    const int mine = slots[min(e0 + (int)(threadIdx.x & 15), n - 1)];
-    auto value = [](uint32_t code, float s) { return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, s, 0)[0]; };
     if (threadIdx.x < 128) {
-        const int blocks = D / 32;
-        for (int i = tid; i < m * blocks; i += 128) {
-            const int e = i / blocks, b = i - e * blocks;
+        for (int e = mine; e < m; e += at_once) {
             const int slot = slots[e0 + e];
             const bool good = (uint32_t)slot < limit;
             const int id = good ? slot >> page_shift : 0, tok = good ? slot & (page - 1) : 0;
             const int64_t place = (int64_t)id * heads + head;
-            uint4 u = *reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(c.k) + (place * page + tok) * (D / 2) + b * 16);
-            float s = __builtin_bit_cast(float, (uint32_t)c.k_byte[(place * page + (tok & ~15)) * (D / 32) + (tok & 3) * (D / 8) + b * 4 + (tok >> 2 & 3)] << 23);
+            uint32_t w = *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(c.k) + (place * page + tok) * (D / 2) + sub * 4);
+            float s = power_of(c.k_byte[(place * page + (tok & ~15)) * (D / 32) + (tok & 3) * (D / 8) + (sub & ~3) + (tok >> 2 & 3)]);
             if (!good) {
-                u = make_uint4(0, 0, 0, 0);
+                w = 0;
                 s = 1.f;
             }
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-            uint4 *dst = reinterpret_cast<uint4 *>(static_cast<uint16_t *>(k_out) + ((int64_t)(e0 + e) * heads + head) * D + b * 32);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const auto p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[j], s, 0), q = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[j], s, 1);
-                const auto r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[j], s, 2), t = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[j], s, 3);
-                dst[j] = make_uint4(pack2<DTYPE>(p[0], p[1]), pack2<DTYPE>(q[0], q[1]), pack2<DTYPE>(r[0], r[1]), pack2<DTYPE>(t[0], t[1]));
-            }
+            *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(k_out) + ((int64_t)(e0 + e) * heads + head) * D + sub * 8) = e2m1_to_16bit<DTYPE>(w, s);
         }
         return;
     }
-    for (int i = tid; i < D / 2; i += 128) {
-        int have = -1;
-        uint64_t x = 0, y = 0;
-        for (int f = 0; f < m; ++f) {
-            const int slot = __builtin_amdgcn_readlane(mine, f);
-            uint32_t out = 0;
-            if ((uint32_t)slot < limit) {
-                const int64_t place = (int64_t)(slot >> page_shift) * heads + head;
-                if ((slot >> 4) != have) {
-                    have = slot >> 4;
-                    const uint4 u = *reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(c.v) + (place * page + (slot & (page - 1) & ~15)) * (D / 2) + i * 16);
-                    x = u.x | (uint64_t)u.y << 32;
-                    y = u.z | (uint64_t)u.w << 32;
+    // neighbouring entries, which mostly lie in the same piece
+    const int each = SUB / at_once;
+    int have = -1;
+    uint64_t x[8];
+    for (int f = mine * each; f < min(m, (mine + 1) * each); ++f) {
+        const int slot = slots[e0 + f];
+        uint4 out = make_uint4(0, 0, 0, 0);
+        if ((uint32_t)slot < limit) {
+            const int64_t place = (int64_t)(slot >> page_shift) * heads + head;
+            if ((slot >> 4) != have) {
+                have = slot >> 4;
+                const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(c.v) + (place * page + (slot & (page - 1) & ~15)) * (D / 2) + sub * 64);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint4 u = p[i];
+                    x[2 * i] = u.x | (uint64_t)u.y << 32;
+                    x[2 * i + 1] = u.z | (uint64_t)u.w << 32;
                 }
-                const float s = __builtin_bit_cast(float, (uint32_t)c.v_byte[place * page + (slot & (page - 1))] << 23);
-                const int at = 4 * (slot & 15);
-                out = pack2<DTYPE>(value((uint32_t)(x >> at) & 15, s), value((uint32_t)(y >> at) & 15, s));
             }
-            reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(v_out) + ((int64_t)(e0 + f) * heads + head) * D)[i] = out;
+            uint32_t w = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w |= ((uint32_t)(x[i] >> (4 * (slot & 15))) & 15) << (4 * i);
+            out = e2m1_to_16bit<DTYPE>(w, power_of(c.v_byte[place * page + (slot & (page - 1))]));
         }
+        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(v_out) + ((int64_t)(e0 + f) * heads + head) * D + sub * 8) = out;
     }
 }
 

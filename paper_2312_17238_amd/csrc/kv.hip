@@ -233,6 +233,7 @@ static int32_t write4(const WriteArgs &args, const Sizes &z, bool turn, hipStrea
     a.kv_blocks = z.p.max_segments * b.subs * b.groups * 2;
     a.q_tokens = a.n_tokens >= 2048 ? 2 : 1;
     const int64_t blocks = (int64_t)a.kv_blocks + (turn ? div_up(a.n_tokens, a.q_tokens) : 0);
+    b.blocks = (uint32_t)blocks;
     const size_t lds = std::max<size_t>({(size_t)tokens * angles * sizeof(double2), (size_t)tokens * a.heads * (a.c.head_dim / 2 + 4), (size_t)a.q_tokens * angles * sizeof(float2)});
     in_pieces(blocks, [&](uint32_t first, unsigned n) {
         a.first = (int32_t)first;
