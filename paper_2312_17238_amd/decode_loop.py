@@ -1,4 +1,4 @@
-"""Whole decoder blocks over requests of any lengths: the paged 8-bit cache and its attention in front of the MoE step.
+"""Whole decoder blocks over requests of any lengths: the paged cache in 8 or 4 bits and its attention in front of the MoE step.
 
     python -m paper_2312_17238_amd.decode_loop [--layers 2] [--requests 4] [--prompt 37] [--tokens 16] [--hidden 256] [--ffn 512] ...
 
@@ -27,6 +27,8 @@ if ROOT not in sys.path:
 import workload as W  # noqa: E402
 from paper_2312_17238_amd import paged  # noqa: E402
 from paper_2312_17238_amd.engine import Stack, layer_config  # noqa: E402
+
+FORMATS = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8, "e2m1": torch.float4_e2m1fn_x2}
 
 
 class Decoder:
@@ -147,12 +149,12 @@ def main(argv=None) -> dict:
     for name, default in (("layers", 2), ("requests", 4), ("prompt", 37), ("tokens", 16), ("hidden", 256), ("ffn", 512), ("q-heads", 4),
                           ("kv-heads", 2), ("head-dim", 64), ("page", 64), ("window", 0), ("cache-slots", 8), ("seed", 0)):
         ap.add_argument("--" + name, type=int, default=default)
-    ap.add_argument("--format", choices=("e4m3", "int8"), default="e4m3")
+    ap.add_argument("--format", choices=tuple(FORMATS), default="e4m3")
     a = ap.parse_args(argv)
     prompts = [max(1, a.prompt - 5 * r) for r in range(a.requests)]      # ragged
     rows = sum(prompts)
     d = Decoder(a.layers, a.hidden, a.ffn, a.q_heads, a.kv_heads, a.head_dim, a.requests, a.prompt + a.tokens, max(rows, a.requests), a.page,
-                torch.float8_e4m3fn if a.format == "e4m3" else torch.int8, a.window, cache_slots=a.cache_slots, seed=a.seed)
+                FORMATS[a.format], a.window, cache_slots=a.cache_slots, seed=a.seed)
     x = W.hidden_ar1(a.seed, 1, rows, a.hidden)[0].to(d.device)
     x = d.step(d.bounds(rows, max(prompts)), x, prompts)
     ends = torch.tensor(prompts).cumsum(0) - 1
