@@ -226,8 +226,10 @@ __device__ __forceinline__ int page_of(const AttendArgs &a, const Item &it, int 
     return (unsigned)id < (unsigned)a.c.n_pages ? id : -1;
 }
 
-// The steps kt0, kt0 + by, ... of 32 rows, straight from memory into registers.
-template <int D>
+// The steps kt0, kt0 + by, ... of 32 rows, straight from memory into registers.  PAIRS: pages of 32 tokens and more, in which a step's two sub-blocks
+// follow each other: where a step lies is then a matter of scalars, and a lane's place in it the same in all steps.  A third of a step's vector
+// instructions went into addresses without it: a prompt of 4096 takes 166 us, 172 by the general way, 512 tokens onto 6000 102 and 106.
+template <int D, bool PAIRS>
 __device__ __forceinline__ void walk4(const AttendArgs &a, const Item &it, int head, const Rows4<D> &r, const Row &row, int pos_a, int pos_z, int kt0, int by, State4<D> &s)
 {
     const int lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5, heads = a.c.kv_heads;
@@ -237,6 +239,7 @@ __device__ __forceinline__ void walk4(const AttendArgs &a, const Item &it, int h
     const int any_lo = a.window > 0 ? max(0, pos_a + 1 - a.window) : 0, any_hi = a.causal ? pos_z + 1 : end;
     const int all_lo = a.window > 0 ? max(0, pos_z + 1 - a.window) : 0, all_hi = a.causal ? pos_a + 1 : end;
     const int kh = (col >> 2) & 1, ktok = 4 * (col >> 3) + (col & 3);     // row `col` of the scores is token 16 kh + ktok of the step
+    const uint32_t lane_k = kh * (SUB * D / 2) + ktok * (D / 2) + 16 * h, lane_kb = kh * (SUB * D / 32) + (col & 3) * (D / 8) + 4 * h, lane_v = h * (SUB * D / 2) + col * 16;
     constexpr int BATCH = 32;       // steps whose pages the lanes hold, two sub-blocks a step
     for (int first = kt0; first < it.kt1; first += by * BATCH) {
         const int n = min(BATCH, div_up(it.kt1 - first, by));
@@ -244,26 +247,41 @@ __device__ __forceinline__ void walk4(const AttendArgs &a, const Item &it, int h
         uint4 k[2][D / 64], v[2][D / 64], vs[2];
         int ks[2][D / 64];
         auto fetch = [&](int j, int u) {
-            const int sub = 2 * (first + by * j), id0 = max(__builtin_amdgcn_readlane(mine, 2 * j), 0), id1 = max(__builtin_amdgcn_readlane(mine, 2 * j + 1), 0);
-            const int in = (1 << a.sub_shift) - 1;
+            const int sub = 2 * (first + by * j), in = (1 << a.sub_shift) - 1;
+            const int id0 = max(__builtin_amdgcn_readlane(mine, 2 * j), 0);
             const uint64_t at0 = ((uint64_t)((uint32_t)id0 * heads + head) << a.sub_shift) + (sub & in);
-            const uint64_t at1 = ((uint64_t)((uint32_t)id1 * heads + head) << a.sub_shift) + ((sub + 1) & in);
-            const uint64_t ak = kh ? at1 : at0, av = h ? at1 : at0;
-            const uint8_t *kp = static_cast<const uint8_t *>(a.c.k) + ak * (SUB * D / 2) + ktok * (D / 2) + 16 * h;
-            const uint8_t *kb = a.c.k_byte + ak * (SUB * D / 32) + (col & 3) * (D / 8) + 4 * h;
-            const uint8_t *vp = static_cast<const uint8_t *>(a.c.v) + av * (SUB * D / 2) + col * 16;
+            if constexpr (PAIRS) {
+                const uint8_t *kp = static_cast<const uint8_t *>(a.c.k) + at0 * (SUB * D / 2), *vp = static_cast<const uint8_t *>(a.c.v) + at0 * (SUB * D / 2);
+                const uint8_t *kb = a.c.k_byte + at0 * (SUB * D / 32), *vb = a.c.v_byte + at0 * SUB;
 #pragma unroll
-            for (int i = 0; i < D / 64; ++i) {
-                k[u][i] = *reinterpret_cast<const uint4 *>(kp + 32 * i);
-                ks[u][i] = *reinterpret_cast<const int *>(kb + 8 * i);
-                v[u][i] = *reinterpret_cast<const uint4 *>(vp + 512 * i);
+                for (int i = 0; i < D / 64; ++i) {
+                    k[u][i] = *reinterpret_cast<const uint4 *>(kp + (lane_k + 32 * i));
+                    ks[u][i] = *reinterpret_cast<const int *>(kb + (lane_kb + 8 * i));
+                    v[u][i] = *reinterpret_cast<const uint4 *>(vp + (lane_v + 512 * i));
+                }
+                vs[u] = *reinterpret_cast<const uint4 *>(vb + (uint32_t)(SUB * h));
+            } else {
+                const int id1 = max(__builtin_amdgcn_readlane(mine, 2 * j + 1), 0);
+                const uint64_t at1 = ((uint64_t)((uint32_t)id1 * heads + head) << a.sub_shift) + ((sub + 1) & in);
+                const uint64_t ak = kh ? at1 : at0, av = h ? at1 : at0;
+                const uint8_t *kp = static_cast<const uint8_t *>(a.c.k) + ak * (SUB * D / 2) + ktok * (D / 2) + 16 * h;
+                const uint8_t *kb = a.c.k_byte + ak * (SUB * D / 32) + (col & 3) * (D / 8) + 4 * h;
+                const uint8_t *vp = static_cast<const uint8_t *>(a.c.v) + av * (SUB * D / 2) + col * 16;
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) {
+                    k[u][i] = *reinterpret_cast<const uint4 *>(kp + 32 * i);
+                    ks[u][i] = *reinterpret_cast<const int *>(kb + 8 * i);
+                    v[u][i] = *reinterpret_cast<const uint4 *>(vp + 512 * i);
+                }
+                vs[u] = *reinterpret_cast<const uint4 *>(a.c.v_byte + av * SUB);
             }
-            vs[u] = *reinterpret_cast<const uint4 *>(a.c.v_byte + av * SUB);
         };
         auto use = [&](int j, int u) {
             const int kt = first + by * j;
             if (kt * KT >= any_hi || (kt + 1) * KT <= any_lo) return;
-            const bool gone = __shfl(mine, 2 * j + h) < 0;
+            // of a pair the second sub-block may lie behind the request's end, where rows see nothing anyway
+            const int id = __builtin_amdgcn_readlane(mine, 2 * j);
+            const bool gone = PAIRS ? id < 0 : (h ? __builtin_amdgcn_readlane(mine, 2 * j + 1) : id) < 0;
             const bool edge = kt * KT < all_lo || (kt + 1) * KT > all_hi || __any(gone);
             const int tok0 = kt * KT + SUB * h;
             Sees mask{see.lo - tok0, gone ? 0 : see.hi - tok0};
@@ -290,7 +308,7 @@ __device__ __forceinline__ void walk4(const AttendArgs &a, const Item &it, int h
 }
 
 // ---- a tile of 32 rows: every wave takes every fourth step of the block's.
-template <int DTYPE, int D>
+template <int DTYPE, int D, bool PAIRS>
 __device__ __forceinline__ void attend4_few(const AttendArgs &a, const Item &it, int head, FewShared<D> &sh)
 {
     constexpr int WAVES = ATTEND_WAVES;
@@ -301,7 +319,7 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, const Item &it,
     load_rows4<DTYPE, D>(a, it, head, row, r);
     State4<D> s;
     clear(s);
-    walk4<D>(a, it, head, r, row, it.ctx + __builtin_amdgcn_readlane(row.tok, 0), it.ctx + __builtin_amdgcn_readlane(row.tok, here - 1), it.kt0 + wave, WAVES, s);
+    walk4<D, PAIRS>(a, it, head, r, row, it.ctx + __builtin_amdgcn_readlane(row.tok, 0), it.ctx + __builtin_amdgcn_readlane(row.tok, here - 1), it.kt0 + wave, WAVES, s);
     // join the waves
     if (h == 0) {
         sh.m[wave][col] = s.m;
@@ -359,7 +377,7 @@ __device__ __forceinline__ void attend4_few(const AttendArgs &a, const Item &it,
 }
 
 // ---- tiles of 32 rows a wave: every wave has its own and takes all steps of the block's.
-template <int DTYPE, int D>
+template <int DTYPE, int D, bool PAIRS>
 __device__ __forceinline__ void attend4_many(const AttendArgs &a, const Item &it, int head, JoinShared &sh)
 {
     constexpr int ROWS = 32 * ATTEND_WAVES;
@@ -371,7 +389,7 @@ __device__ __forceinline__ void attend4_many(const AttendArgs &a, const Item &it
     if (row0 < rows) {
         Rows4<D> r;
         load_rows4<DTYPE, D>(a, it, head, row, r);
-        walk4<D>(a, it, head, r, row, it.ctx + __builtin_amdgcn_readlane(row.tok, 0), it.ctx + __builtin_amdgcn_readlane(row.tok, min(31, rows - 1 - row0)), it.kt0, 1, s);
+        walk4<D, PAIRS>(a, it, head, r, row, it.ctx + __builtin_amdgcn_readlane(row.tok, 0), it.ctx + __builtin_amdgcn_readlane(row.tok, min(31, rows - 1 - row0)), it.kt0, 1, s);
     }
     const bool whole = it.part < 0;
     float *ml = a.part_many + (int64_t)a.p.parts_many * heads * ROWS * D;
@@ -399,7 +417,7 @@ __device__ __forceinline__ void attend4_many(const AttendArgs &a, const Item &it
     if (!whole && all_parts_done(a.p.joins_many + it.join * heads + head, it.parts, sh.last)) join_tile<DTYPE, D, ROWS>(a, it, head, parts, ml, sh);
 }
 
-template <int DTYPE, int D>
+template <int DTYPE, int D, bool PAIRS>
 __global__ void __launch_bounds__(64 * ATTEND_WAVES, D <= 128 ? 2 : 1) k_kv4_attend(AttendArgs a)
 {
     __shared__ union {
@@ -410,14 +428,14 @@ __global__ void __launch_bounds__(64 * ATTEND_WAVES, D <= 128 ? 2 : 1) k_kv4_att
     if ((int)blockIdx.x < a.many_blocks) {
         const int i = blockIdx.x / heads;
         const Item it = item_at(a.p.many + i);
-        if (i < a.p.head->many) attend4_many<DTYPE, D>(a, it, blockIdx.x - i * heads, sh.many);
+        if (i < a.p.head->many) attend4_many<DTYPE, D, PAIRS>(a, it, blockIdx.x - i * heads, sh.many);
     } else {
         const int b = blockIdx.x - a.many_blocks, i = b / heads;
         const int first = a.p.few_first[i], last = a.p.few_first[i + 1];
         if (i >= a.p.head->few_blocks) return;
         for (int k = first; k < last; ++k) {
             if (k > first) __syncthreads();          // the item before is done with LDS
-            attend4_few<DTYPE, D>(a, item_at(a.p.few + k), b - i * heads, sh.few);
+            attend4_few<DTYPE, D, PAIRS>(a, item_at(a.p.few + k), b - i * heads, sh.few);
         }
     }
 }

@@ -328,10 +328,12 @@ static void launch_attend4(const AttendArgs &a, int D, bool decode, dim3 grid, h
         }
         return;
     }
+    const dim3 block(64 * ATTEND_WAVES);
+    const bool pairs = a.sub_shift > 0;
     switch (D) {
-    case 64: hipLaunchKernelGGL((k_kv4_attend<DTYPE, 64>), grid, dim3(64 * ATTEND_WAVES), 0, s, a); break;
-    case 128: hipLaunchKernelGGL((k_kv4_attend<DTYPE, 128>), grid, dim3(64 * ATTEND_WAVES), 0, s, a); break;
-    default: hipLaunchKernelGGL((k_kv4_attend<DTYPE, 256>), grid, dim3(64 * ATTEND_WAVES), 0, s, a); break;
+    case 64: pairs ? k_kv4_attend<DTYPE, 64, true><<<grid, block, 0, s>>>(a) : k_kv4_attend<DTYPE, 64, false><<<grid, block, 0, s>>>(a); break;
+    case 128: pairs ? k_kv4_attend<DTYPE, 128, true><<<grid, block, 0, s>>>(a) : k_kv4_attend<DTYPE, 128, false><<<grid, block, 0, s>>>(a); break;
+    default: pairs ? k_kv4_attend<DTYPE, 256, true><<<grid, block, 0, s>>>(a) : k_kv4_attend<DTYPE, 256, false><<<grid, block, 0, s>>>(a); break;
     }
 }
 
