@@ -13,7 +13,13 @@
 //
 // Values.  Codes become fp16 (exact) and have one scale a token, 2^(b - 127), which goes into the exponent: with t = scale log2(e) (q.k) + b
 // the weight of a token's codes is 2^(t - m), m the running maximum of t, and the sum of the probabilities is that of the weights
-// times 2^(128 - b) (a factor that cancels).  b is from 82 to 172, so neither leaves fp32.
+// times 2^(128 - b) (a factor that cancels).  b is from 82 to 172, so neither leaves fp32; t is rounded by 2^-17 at that size, a weight by as much.
+//
+// A prompt of 4096 (32 query and 8 kv heads of 128): 166 us, 0.83 PFLOP/s, 71 % of a large library product, by 8-bit codes 163 to 173.  Every wave reads
+// its keys and values for itself, 133 bytes a token and head, out of the caches; nothing is shared through LDS and no wave waits for another.  By way of
+// LDS (keys as they are, values converted once to fp16, scales as numbers) the same prompt took 174 us, with heads of 256 459 instead
+// of 393.  Vector unit 69 % of the time, matrix unit 32 %: the two hardly overlap at two waves a SIMD, so what a step's 190 vector
+// instructions are is what it costs: 32 conversions of values, 16 each of scale, maximum, difference, exponential and sum.
 #pragma once
 #include "kernels_kv_attend.h"
 

@@ -5,6 +5,11 @@
 // lanes of four neighbouring rows read 4 x D / 2 bytes in one piece and a lane's four tiles have their scales in one word; output row m of
 // tile 2 i + e is dim 32 i + 2 m + e.  A lane of quarter g holds 32 dims of a query: g's, of heads of 256 those of g + 4 too.  Heads of 64 have two
 // blocks of dims, so that an instruction takes two digits at once, one in the lower half of its quarters and one in the upper.
+//
+// Memory is the bound, 133 bytes a token and kv head: 64 requests over 2000 tokens each 26.6 us (137 MB, 5.2 TB/s), 64 over 8000 98.8 (5.5 TB/s), one
+// over 524000 106 (5.3 TB/s).  Below that it is starts and joins: 64 requests over 500 to 8000 50 us (176 MB; a plain read of as much 35.6, these
+// loads without anything else 44), one over 131000 36.7 (139 MB; 29.9 and 38), of which a join of 64 parts is 4.  The 32-row kernel takes 59
+// and 43 for these.  Two steps ahead instead of one: 66 and 45, for the registers.
 #pragma once
 #include "kernels_kv4_attend.h"
 #include "kernels_kv_decode.h"
@@ -13,7 +18,8 @@ namespace moe {
 namespace kv {
 
 // Joining the parts of a tile's rows, in the parts' order.  What this costs is not its bytes but one wait behind the other, those for code that is not in
-// the instruction cache among them: one short loop without a branch inside, which takes a part's maximum, sum and outputs in one go.
+// the instruction cache among them: one short loop without a branch inside, which takes a part's maximum, sum and outputs in one go.  One token over 2000
+// (3 parts) takes 11.3 us, 12.0 with join_parts, whose loops are unrolled; over 131000 (64 parts) 36.7 and 38.6; without any join 8.7 and 29.
 struct Join4Shared {
     float4 sum[64 * DECODE_WAVES];      // of a thread
     float2 ml[64 * DECODE_WAVES];
