@@ -18,8 +18,8 @@
 // A prompt of 4096 (32 query and 8 kv heads of 128): 166 us, 0.83 PFLOP/s, 71 % of a large library product, by 8-bit codes 163 to 173.  Every wave reads
 // its keys and values for itself, 133 bytes a token and head, out of the caches; nothing is shared through LDS and no wave waits for another.  By way of
 // LDS (keys as they are, values converted once to fp16, scales as numbers) the same prompt took 174 us, with heads of 256 459 instead
-// of 393.  Vector unit 69 % of the time, matrix unit 32 %: the two hardly overlap at two waves a SIMD, so what a step's 190 vector
-// instructions are is what it costs: 32 conversions of values, 16 each of scale, maximum, difference, exponential and sum.
+// of 393.  Vector unit 69 % of the time, matrix unit 34 %: the two hardly overlap at two waves a SIMD, so what a step's 195 vector
+// instructions are is what it costs: 32 conversions of values, 44 for bytes and inverses of scales, 16 each of scale, difference, exponential and sum.
 #pragma once
 #include "kernels_kv_attend.h"
 
@@ -234,7 +234,8 @@ __device__ __forceinline__ int page_of(const AttendArgs &a, const Item &it, int 
 
 // The steps kt0, kt0 + by, ... of 32 rows, straight from memory into registers.  PAIRS: pages of 32 tokens and more, in which a step's two sub-blocks
 // follow each other: where a step lies is then a matter of scalars, and a lane's place in it the same in all steps.  A third of a step's vector
-// instructions went into addresses without it: a prompt of 4096 takes 166 us, 172 by the general way, 512 tokens onto 6000 102 and 106.
+// instructions went into addresses without it: a prompt of 4096
+// takes 165 us, 172 by the general way, 512 tokens onto 6000 103 and 106.
 template <int D, bool PAIRS>
 __device__ __forceinline__ void walk4(const AttendArgs &a, const Item &it, int head, const Rows4<D> &r, const Row &row, int pos_a, int pos_z, int kt0, int by, State4<D> &s)
 {
@@ -292,7 +293,10 @@ __device__ __forceinline__ void walk4(const AttendArgs &a, const Item &it, int h
             const int tok0 = kt * KT + SUB * h;
             Sees mask{see.lo - tok0, gone ? 0 : see.hi - tok0};
             uint4 b = vs[u];
-            if (edge) b = keep_scales(b, any_lo - tok0, gone ? 0 : end - tok0);
+            if (edge) {
+                asm volatile("");       // a branch, as in step4
+                b = keep_scales(b, any_lo - tok0, gone ? 0 : end - tok0);
+            }
             int sk[D / 64];
 #pragma unroll
             for (int i = 0; i < D / 64; ++i) sk[i] = ks[u][i] >> (8 * (col >> 3));
