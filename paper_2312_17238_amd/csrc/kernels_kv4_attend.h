@@ -47,7 +47,8 @@ __device__ __forceinline__ v8i operand(uint4 k) { return v8i{(int)k.x, (int)k.y,
 __device__ __forceinline__ v8i operand(v6u q) { return v8i{(int)q[0], (int)q[1], (int)q[2], (int)q[3], (int)q[4], (int)q[5], 0, 0}; }
 
 // 32 numbers of a query as digits.  top: the largest of their bits without sign.  The digits' scale bytes, first digit lowest, are
-// for numbers in units of 2^(row - 127), row the exponent of the query's largest number, times 2^-14.
+// for numbers in units of 2^(row - 127), row the exponent of the query's largest number, times 2^-14.  A block is written in units of 2^-100 of
+// that at least, so that its scales stay above 0: what is below has the small digits, or none, that it then comes to.
 struct Digits {
     v6u d[DIGITS];
     int scale;
@@ -56,7 +57,7 @@ struct Digits {
 __device__ __forceinline__ Digits digits_of(float (&x)[32], uint32_t top, int row)
 {
     Digits r;
-    const int e = max((int)(top >> 23), 1);
+    const int e = max(max((int)(top >> 23), 1), row - 100);
 #pragma unroll
     for (int j = 0; j < 32; ++j) x[j] = ldexpf(x[j], 127 - e);      // below 2 in size
 #pragma unroll
@@ -75,7 +76,7 @@ __device__ __forceinline__ Digits digits_of(float (&x)[32], uint32_t top, int ro
             for (int j = 0; j < 32; ++j) x[j] = fmaf(x[j], 32.f, -n[j]);
         }
     }
-    const int b = 127 + 14 + max(e - row, -100);
+    const int b = 127 + 14 + e - row;
     r.scale = b | (b - 5) << 8 | (b - 10) << 16 | (b - 15) << 24;
     return r;
 }
