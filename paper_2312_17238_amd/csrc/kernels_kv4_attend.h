@@ -197,7 +197,8 @@ __device__ __forceinline__ void step4(State4<D> &s, const Rows4<D> &r, const uin
 #pragma unroll
     for (int i = 1; i < 16; ++i) t = fmaxf(t, z[i]);
     t = max_halves(t);
-    if (__any(t > s.m + RISE)) {
+    // the difference, which is exact where it matters: m + RISE is rounded up to 16 above m for scores of 2^27, and a weight of 2^16 is no fp16 number
+    if (__any(t - s.m > RISE)) {
         const float m = fmaxf(s.m, t);
         const float f = m == -INFINITY ? 1.f : exp2f(s.m - m);
         s.l = m == -INFINITY ? s.l : times_two_to(s.l, s.m - m);

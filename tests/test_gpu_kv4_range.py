@@ -1,14 +1,30 @@
 """Attention over the cache in 4 bits where numbers are far apart: blocks of a query, scores that are large, single tokens beside very many, and what is left of a score's
 last bits. Every form of it: single tokens, tiles of few rows, tiles of many."""
+import math
+
 import numpy as np
 import pytest
 import torch
 
 import kv4_reference as R4
 from paper_2312_17238_amd import paged
-from test_gpu_kv4 import DEV, Pool, fill, half_step, planned
+from test_gpu_kv4 import DEV, FOUR, Pool, fill, half_step, i32, planned
 
 pytestmark = pytest.mark.gpu
+
+
+def pack(keys, values, heads):
+    """A cache whose pages hold these codes [pages][page][dim] in all heads, all scales 1."""
+    n, page, dim = keys.shape
+    c = paged.Cache.empty(n, heads, dim, page, FOUR, DEV)
+    k = keys[..., 0::2] | (keys[..., 1::2] << 4)
+    v = values.reshape(n, page // 16, 16, dim).swapaxes(2, 3)
+    v = v[..., 0::2] | (v[..., 1::2] << 4)
+    for t, x in ((c.k, k), (c.v, v)):
+        t.view(torch.uint8).copy_(torch.from_numpy(np.ascontiguousarray(x)).unsqueeze(1).expand(*t.shape))
+    for t in (c.k_scale, c.v_scale):
+        t.view(torch.uint8).fill_(127)
+    return c
 
 
 @pytest.mark.parametrize("lens,new", [([300, 41], [1, 1]), ([300, 41], [20, 5]), ([300, 100], [70, 40])])
@@ -42,3 +58,37 @@ def test_blocks_of_a_query_far_below_its_largest(lens, new, dim, gap):
             assert (np.abs(out[at:at + m, h] - want) <= slack + half_step(want, p.dtype) * 1.01 + 2 * extra * 12).all()
             assert (np.abs(lse[at:at + m, h] - wl) <= off + extra).all()
         at += m
+
+
+FORMS = [([1], 1), ([3], 2), ([20], 1), ([70], 2), ([130], 1)]      # new tokens, query heads a kv head
+
+
+@pytest.mark.parametrize("new,group", FORMS)
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("power", [20, 24, 26, 27, 28, 30])
+def test_scores_whose_last_bit_is_large(new, group, dim, power):
+    """Two tokens that one wave meets one after the other, with scores of 2^power (in powers of two) and one to four of such a number's last bits between
+    them. Their values are alike, so the output is that value whatever the bits do."""
+    step = 2.0 ** (power - 23)
+    for first in range(4):
+        for second in range(first + 1, 5):
+            keys, values = np.zeros((6, 64, dim), np.uint8), np.zeros((6, 64, dim), np.uint8)
+            values[0, 0] = values[4, 0] = 2
+            keys[0, 0, 0] = keys[4, 0, 0] = 2
+            keys[0, 0, 32], keys[4, 0, 32] = (0, 2, 4, 5, 6)[first], (0, 2, 4, 5, 6)[second]      # 0, 1, 2, 3, 4
+            c = pack(keys, values, 2)
+            n = sum(new)
+            s = paged.Step(1, n, n, 6, 6, 64, 2 * group, 2, dim)
+            table = torch.arange(6, dtype=torch.int32, device=DEV)[None].contiguous()
+            s.plan(i32([384 - n]), i32(new), table, i32([5, 4, 3][:(384 - -(-(384 - n) // 64) * 64) // 64] + [0]), i32([6 - -(-(384 - n) // 64)]))
+            assert s.status.tolist() == [0] and table.tolist() == [list(range(6))]
+            q = torch.zeros(n, 2 * group, dim, dtype=torch.bfloat16, device=DEV)
+            q[..., 0], q[..., 32] = 2.0 ** power, step
+            out, lse = paged.attend(c, s, q, math.log(2), with_lse=True)
+            late = torch.arange(384 - n, 384, device=DEV) >= 256           # rows that see the second token, too; the others see the first
+            top = torch.where(late, float(second), float(first)).double() * step + 2.0 ** power
+            # all other tokens' weights are 0; these two's are rounded to fp16 (2^-11), their sum is not, and bf16's half step is 2^-8 at 1
+            assert ((out.double() - 1).abs() <= 2.0 ** -8).all(), (first, second)
+            # in a score's last bits: the factor 1, what is added to it 1/2, the maximum 1/2, the logarithm added 1/2, ln 2 and the product 3/4, and the sum of
+            # two weights is two at most
+            assert ((lse.double() / math.log(2) - top[:, None]).abs() <= 4 * step + 1 + 2.0 ** -6).all(), (first, second)
