@@ -164,9 +164,10 @@ typedef struct {
 /* Attention of a step's rows: out = sum_j softmax(scale * q.k_j) v_j over the cached tokens that the row sees.  A row that sees none gets
  * 0 and lse -inf.  Table entries outside the cache are skipped as if they were masked.  Deterministic: how the work is split follows from the lengths alone.
  * Scores, maxima, sums and outputs are held in fp32, codes are exact.  Rounded to fewer bits are: the weights that values are multiplied with, to fp16
- * (2^-11 of a weight at most; with fp16 outputs the distance from 64 bits is 1.3 times that of fp32 weights, with bf16 outputs the same), and bf16
- * queries, to fp16 after a power of two is taken off each row (what is 2^38 below a row's largest is dropped).  Both let the matrix units
- * work on 16-bit operands.  With a cache in 4 bits the weights are rounded alike, and queries of either type to 21 bits: a number is off by 2^-20 of the
+ * (2^-11 of a weight at most; with fp16 outputs the distance from 64 bits is 1.3 times that of fp32 weights, with bf16 outputs the same.  A weight, which is a
+ * probability times its value's scale, that is below 2^-14 of the largest that a wave has met is off by 2^-25 of the largest instead, in 4 bits one
+ * below 2^-21 by 2^-32: n tokens far behind one lose n times that of the output), and bf16 queries, to fp16 after a power of two is taken off each row (what is 2^38 below a row's largest is dropped).  Both let the matrix units
+ * work on 16-bit operands.  With a cache in 4 bits queries of either type are rounded to 21 bits: a number is off by 2^-20 of the
  * power of two above the largest of its 32 dims (0..31, 32..63, ...) at most, which is nothing for those above 2^-9 of it in fp16 and 2^-12 in bf16
  * (of 2^-99 of the row's largest number where those dims' is smaller still).
  * (fp16 outputs are 2.0 to 2.4e-4 from 64 bits where fp32 throughout is 2.0e-4, bf16 ones the same.)  A row whose query holds an infinity or NaN is NaN. */

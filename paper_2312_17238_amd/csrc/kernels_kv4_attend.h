@@ -12,7 +12,7 @@
 // do, but a block's products are added with 13 bits or so below the largest, which numbers of very different sizes need more than: 2^-16 of the sum.)
 //
 // Values.  Codes become fp16 (exact) and have one scale a token, 2^(b - 127), which goes into the exponent: with t = scale log2(e) (q.k) + b
-// the weight of a token's codes is 2^(t - m), m the running maximum of t, and the sum of the probabilities is that of the weights
+// the weight of a token's codes is 2^(t - m), m the running maximum of t less 7 (see LIFT), and the sum of the probabilities is that of the weights
 // times 2^(128 - b) (a factor that cancels).  b is from 82 to 172, so neither leaves fp32; t is rounded by 2^-17 at that size, a weight by as much.
 //
 // A prompt of 4096 (32 query and 8 kv heads of 128): 166 us, 0.83 PFLOP/s, 71 % of a large library product, by 8-bit codes 163 to 173.  Every wave reads
@@ -31,6 +31,11 @@ typedef unsigned int v6u __attribute__((ext_vector_type(6)));
 typedef float v32f __attribute__((ext_vector_type(32)));
 
 constexpr int DIGITS = 4;
+
+// Weights are taken relative to 2^-LIFT of the largest that a row had when its sums were last scaled, and may rise to 2^REACH before they are again:
+// nearly all of what fp16 holds. A weight down to 2^-21 of that largest is rounded by 2^-11 of itself, a smaller one by 2^-32 of the largest, so
+// that a million tokens behind one of a much higher score lose 2^-12 of the output at most (with weights of 1 for the largest: 2^-25 and 3 %).
+constexpr float LIFT = 7.f, REACH = 15.f;
 
 // Eight codes of a word as fp16 numbers.
 __device__ __forceinline__ v8h e2m1_to_half(uint32_t w)
@@ -197,9 +202,9 @@ __device__ __forceinline__ void step4(State4<D> &s, const Rows4<D> &r, const uin
 #pragma unroll
     for (int i = 1; i < 16; ++i) t = fmaxf(t, z[i]);
     t = max_halves(t);
-    // the difference, which is exact where it matters: m + RISE is rounded up to 16 above m for scores of 2^27, and a weight of 2^16 is no fp16 number
-    if (__any(t - s.m > RISE)) {
-        const float m = fmaxf(s.m, t);
+    // the difference, which is exact where it matters: m + REACH is rounded up to 16 above m for scores of 2^27, and a weight of 2^16 is no fp16 number
+    if (__any(t - s.m > REACH)) {
+        const float m = fmaxf(s.m, t - LIFT);
         const float f = m == -INFINITY ? 1.f : exp2f(s.m - m);
         s.l = m == -INFINITY ? s.l : times_two_to(s.l, s.m - m);
 #pragma unroll

@@ -259,8 +259,8 @@ struct Decode4 {
 #pragma unroll
         for (int t = 1; t < 4; ++t) s = fmaxf(fmaxf(s, fmaxf(z[t][0], z[t][1])), fmaxf(z[t][2], z[t][3]));
         s = max_quarters(s);
-        if (__any(s - m > RISE)) {      // as in step4
-            const float up = fmaxf(m, s), f = up == -INFINITY ? 1.f : exp2f(m - up);
+        if (__any(s - m > REACH)) {     // as in step4
+            const float up = fmaxf(m, s - LIFT), f = up == -INFINITY ? 1.f : exp2f(m - up);
             l = up == -INFINITY ? l : times_two_to(l, m - up);
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) o[i] *= f;

@@ -92,3 +92,35 @@ def test_scores_whose_last_bit_is_large(new, group, dim, power):
             # in a score's last bits: the factor 1, what is added to it 1/2, the maximum 1/2, the logarithm added 1/2, ln 2 and the product 3/4, and the sum of
             # two weights is two at most
             assert ((lse.double() / math.log(2) - top[:, None]).abs() <= 4 * step + 1 + 2.0 ** -6).all(), (first, second)
+
+
+@pytest.mark.parametrize("new,group", FORMS)
+@pytest.mark.parametrize("dim,dtype", [(64, torch.float16), (128, torch.bfloat16), (256, torch.float16)])
+def test_many_tokens_behind_one(new, group, dim, dtype):
+    """131000 tokens with a score of 0 behind one of 17.5: each has e^-17.5 (2^-25.2) of its weight, all of them 0.3 % of the sum."""
+    m, n, heads, peak = sum(new), 131000, 64, 17.5
+    keys, values = np.zeros((2, 64, dim), np.uint8), np.zeros((2, 64, dim), np.uint8)
+    keys[0, 0, 0] = 7                                   # 6 in the first dim of the first token
+    values[:, :, :dim // 2] = 2                         # all others: 1 in the first half
+    values[0, 0, :dim // 2], values[0, 0, dim // 2:] = 0, 2
+    c = pack(keys, values, heads)
+    width = -(-n // 64)
+    table = torch.ones(1, width, dtype=torch.int32, device=DEV)
+    table[0, 0] = 0
+    s = paged.Step(1, m, m, width, 2, 64, heads * group, heads, dim)
+    free = width - -(-(n - m) // 64)
+    s.plan(i32([n - m]), i32(new), table, i32([1] * 4), i32([free]))
+    assert s.status.tolist() == [0]
+    q = torch.zeros(m, heads * group, dim, dtype=dtype, device=DEV)
+    q[..., 0] = 1
+    out, lse = (x.double().cpu().numpy() for x in paged.attend(c, s, q, peak / 6, with_lse=True))
+    tail = np.arange(n - m, n, dtype=np.float64)[:, None, None]         # other tokens that a row sees
+    want = np.broadcast_to(tail / (tail + math.exp(peak)), out[..., :dim // 2].shape)
+    # Each weight is off by 2^-11 of itself or 2^-32 of the wave's largest, the score by three roundings of 26 (in powers of two), and sums of
+    # n numbers in fp32 by n 2^-24, in the weights and in what they are divided by.
+    allowed = tail * 2.0 ** -32 + want * (2.0 ** -11 + 3 * 26 * 2.0 ** -24 + 2 * n * 2.0 ** -24) + half_step(want, dtype) * 1.01
+    err = np.abs(out[..., :dim // 2] - want)
+    assert (err <= allowed).all(), float((err / allowed).max())
+    one = 1 - want
+    assert (np.abs(out[..., dim // 2:] - one) <= one * (2.0 ** -11 + 2.0 ** -17 + 2 * n * 2.0 ** -24) + half_step(one, dtype) * 1.01).all()
+    assert (np.abs(lse - np.log(tail[..., 0] + math.exp(peak))) <= 2.0 ** -17 + n * 2.0 ** -24).all()
