@@ -11,9 +11,10 @@
 // off by at most 2^-20 of the power of two above the largest of its 32 dims, everything else of a score is fp32.  (As e4m3 numbers three parts would
 // do, but a block's products are added with 13 bits or so below the largest, which numbers of very different sizes need more than: 2^-16 of the sum.)
 //
-// Values.  Codes become fp16 (exact) and have one scale a token, 2^(b - 127), which goes into the exponent: with t = scale log2(e) (q.k) + b
-// the weight of a token's codes is 2^(t - m), m the running maximum of t less 7 (see LIFT), and the sum of the probabilities is that of the weights
-// times 2^(128 - b) (a factor that cancels).  b is from 82 to 172, so neither leaves fp32; t is rounded by 2^-17 at that size, a weight by as much.
+// Values.  Twice a code becomes fp16 (exact), and its token has one scale, 2^(b - 127), half of which goes into the exponent: with t = scale log2(e) (q.k)
+// + b - 128 the weight of a token's codes is 2^(t - m), m the running maximum of t less 7 (see LIFT), and the sum of the probabilities is that of the weights
+// times 2^(128 - b).  b is from 82 to 172, so neither leaves fp32.  b - 128 is the byte with its highest bit turned over, as a signed one: t is of the size of the score
+// and of the scale's exponent, and rounded as numbers of that size are (with b itself, which needs no turning over, by 2^-17 even where both are small).
 //
 // A prompt of 4096 (32 query and 8 kv heads of 128): 166 us, 0.83 PFLOP/s, 71 % of a large library product, by 8-bit codes 163 to 173.  Every wave reads
 // its keys and values for itself, 133 bytes a token and head, out of the caches; nothing is shared through LDS and no wave waits for another.  By way of
@@ -37,14 +38,14 @@ constexpr int DIGITS = 4;
 // that a million tokens behind one of a much higher score lose 2^-12 of the output at most (with weights of 1 for the largest: 2^-25 and 3 %).
 constexpr float LIFT = 7.f, REACH = 15.f;
 
-// Eight codes of a word as fp16 numbers.
+// Eight codes of a word as fp16 numbers, times two.
 __device__ __forceinline__ v8h e2m1_to_half(uint32_t w)
 {
     union { v8h v; v2h p[4]; } r;
-    r.p[0] = __builtin_bit_cast(v2h, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.f, 0));
-    r.p[1] = __builtin_bit_cast(v2h, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.f, 1));
-    r.p[2] = __builtin_bit_cast(v2h, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.f, 2));
-    r.p[3] = __builtin_bit_cast(v2h, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.f, 3));
+    r.p[0] = __builtin_bit_cast(v2h, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 2.f, 0));
+    r.p[1] = __builtin_bit_cast(v2h, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 2.f, 1));
+    r.p[2] = __builtin_bit_cast(v2h, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 2.f, 2));
+    r.p[3] = __builtin_bit_cast(v2h, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 2.f, 3));
     return r.v;
 }
 
@@ -97,7 +98,8 @@ __device__ __forceinline__ uint4 keep_scales(uint4 v, int lo, int hi)
     return make_uint4(k.x | (z.x ^ 0x7F7F7F7Fu), k.y | (z.y ^ 0x7F7F7F7Fu), k.z | (z.z ^ 0x7F7F7F7Fu), k.w | (z.w ^ 0x7F7F7F7Fu));
 }
 
-__device__ __forceinline__ float byte_of(uint32_t w, int i) { return (float)((w >> (8 * i)) & 255u); }
+// b - 128 of byte i, from the word with every byte's highest bit turned over
+__device__ __forceinline__ float exponent_of(uint32_t w, int i) { return (float)(int8_t)(w >> (8 * i)); }
 // 2^(128 - b) of byte i, from the word's complement
 __device__ __forceinline__ float inverse_of(uint32_t nw, int i) { return __builtin_bit_cast(float, ((nw >> (8 * i)) & 255u) << 23); }
 
@@ -192,7 +194,7 @@ __device__ __forceinline__ void step4(State4<D> &s, const Rows4<D> &r, const uin
     }
     const uint32_t b[4] = {vs.x, vs.y, vs.z, vs.w};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) z[i] = fmaf(z[i], r.factor, byte_of(b[i / 4], i % 4));
+    for (int i = 0; i < 16; ++i) z[i] = fmaf(z[i], r.factor, exponent_of(b[i / 4] ^ 0x80808080u, i % 4));
     if (edge) {
         asm volatile("");               // a branch: as selections this would be worked out for every step
 #pragma unroll
@@ -319,9 +321,6 @@ __device__ __forceinline__ void walk4(const AttendArgs &a, const Item &it, int h
         }
     }
     s.l += __shfl_xor(s.l, 32);
-    // to the form that parts have: m without the bytes' offset, l as the sum of the probabilities
-    s.m -= 127.f;
-    s.l *= 0.5f;
 }
 
 // ---- a tile of 32 rows: every wave takes every fourth step of the block's.

@@ -246,7 +246,7 @@ struct Decode4 {
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) z[t][i] = fmaf(z[t][i], w.factor, byte_of(b[t], i));
+            for (int i = 0; i < 4; ++i) z[t][i] = fmaf(z[t][i], w.factor, exponent_of(b[t] ^ 0x80808080u, i));
         if (edge) {
             asm volatile("");
             const int lo = w.see.lo - tok0, hi = dead ? 0 : min(w.see.hi, w.part_hi) - tok0;
@@ -357,9 +357,7 @@ struct Decode4 {
         }
         if (more) queries(next, after);
 
-        // join the waves; m without the bytes' offset, l as the sum of the probabilities
-        m -= 127.f;
-        l *= 0.5f;
+        // join the waves
         l += __shfl_xor(l, 16);
         l += __shfl_xor(l, 32);
         if (g == 0) {

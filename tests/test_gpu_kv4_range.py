@@ -124,3 +124,31 @@ def test_many_tokens_behind_one(new, group, dim, dtype):
     one = 1 - want
     assert (np.abs(out[..., dim // 2:] - one) <= one * (2.0 ** -11 + 2.0 ** -17 + 2 * n * 2.0 ** -24) + half_step(one, dtype) * 1.01).all()
     assert (np.abs(lse - np.log(tail[..., 0] + math.exp(peak))) <= 2.0 ** -17 + n * 2.0 ** -24).all()
+
+
+@pytest.mark.parametrize("new", [[1] * 300, [4] * 40, [20, 300, 40], [300, 1, 500]])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_the_sum_of_one_token_is_its_score(new, dim):
+    """A window of one: lse is the row's own score, to fp32's rounding of numbers of its size, whatever the value's scale is."""
+    p = Pool(len(new), -(-max(new) // 16) + 2, page=16, q_heads=4, kv_heads=2, dim=dim, window=1, seed=dim)
+    lens = [n + 5 for n in new]
+    fill(p, lens, k_exp=(-1, 1), v_exp=(1, 3))
+    s = planned(p, lens, new)
+    # multiples of 1/4 up to 2: four digits, products and sums are exact
+    q = torch.from_numpy(p.rng.integers(-8, 9, (sum(new), 4, dim)) / 4.0).half().to(DEV)
+    k, kb, _, _ = p.tensors()
+    scores = np.zeros((sum(new), 4))
+    qd, at = q.double().cpu().numpy(), 0
+    for r, (n, m) in enumerate(zip(lens, new)):
+        ids = p.table[r, :-(-n // 16)].cpu().numpy()
+        for h in range(4):
+            scores[at:at + m, h] = (qd[at:at + m, h] * R4.keys(k[ids, h // 2], kb[ids, h // 2]).reshape(-1, dim)[n - m:n]).sum(-1)
+        at += m
+    # the largest score becomes one power of two; the scale in fp32, as the call takes it
+    scale = float(np.float32(math.log(2) / np.abs(scores).max()))
+    _, lse = paged.attend(p.cache, s, q, scale, with_lse=True)
+    # In units of 2^-24, in powers of two: the score's two products 2.5, the value's exponent (up to 3) added to it 2, the maximum lowered by 7 (half a step
+    # below 16) 8, taken off 8, exp2 (a step of the result, 2 log2(e)) 3, its product with the value's inverse 1.5, log2 (a step of a number below 16) 16, the maximum added 8,
+    # ln 2 and the product 2: 51.
+    err = np.abs(lse.double().cpu().numpy() - scale * scores)
+    assert err.max() <= 51 * 2.0 ** -24 * math.log(2), err.max()
