@@ -8,7 +8,7 @@ import torch
 
 import kv4_reference as R4
 from paper_2312_17238_amd import paged
-from test_gpu_kv4 import DEV, FOUR, Pool, fill, half_step, i32, planned
+from test_gpu_kv4 import DEV, FOUR, Pool, check_attend, fill, half_step, i32, planned
 
 pytestmark = pytest.mark.gpu
 
@@ -152,3 +152,35 @@ def test_the_sum_of_one_token_is_its_score(new, dim):
     # ln 2 and the product 2: 51.
     err = np.abs(lse.double().cpu().numpy() - scale * scores)
     assert err.max() <= 51 * 2.0 ** -24 * math.log(2), err.max()
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("window", [0, 50])
+@pytest.mark.parametrize("lens,new", [([300, 9000], [5, 3]), ([9000, 64, 1], [8, 2, 1]), ([2000, 33], [1, 1])])
+def test_all_tokens_are_seen_by_few_rows(lens, new, window, dim):
+    """Steps of at most sixteen rows a request without a causal mask, with and without a window."""
+    p = Pool(len(lens), -(-max(lens) // 64) + 1, page=64, dim=dim, q_heads=4, kv_heads=2, causal=False, window=window, seed=sum(lens))
+    fill(p, lens)
+    s = planned(p, lens, new, spare=1)
+    q = p.rows(sum(new) + 1, 4, spread=0.5)
+    out, lse = paged.attend(p.cache, s, q, with_lse=True)
+    check_attend(p, q, out, lse, lens, new, 1 / math.sqrt(dim))
+
+
+@pytest.mark.parametrize("new", [[1, 1], [20, 3], [70, 40], [5, 70]])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("gone", [0, 1])
+def test_a_request_that_is_served_and_sees_nothing(new, dim, gone):
+    """Tables that name no page of the cache: rows get 0 and -inf, in one piece and in several that are joined, and the other request what it gets anyway."""
+    lens = [9000, 200]
+    p = Pool(2, 564, dim=dim, page=16, q_heads=4, kv_heads=2, seed=new[0])
+    fill(p, lens)
+    s = planned(p, lens, new)
+    q = p.rows(sum(new), 4)
+    want = paged.attend(p.cache, s, q, with_lse=True)
+    p.table[gone] = torch.tensor([-1, p.n_pages, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32, device=DEV).repeat(141)
+    out, lse = paged.attend(p.cache, s, q, with_lse=True)
+    mine = slice(0, new[0]) if gone == 0 else slice(new[0], sum(new))
+    others = slice(new[0], sum(new)) if gone == 0 else slice(0, new[0])
+    assert (out[mine] == 0).all() and (lse[mine] == -math.inf).all()
+    assert torch.equal(out[others], want[0][others]) and torch.equal(lse[others], want[1][others])
