@@ -28,7 +28,7 @@ import workload as W  # noqa: E402
 from paper_2312_17238_amd import paged  # noqa: E402
 from paper_2312_17238_amd.engine import Stack, layer_config  # noqa: E402
 
-FORMATS = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8, "e2m1": torch.float4_e2m1fn_x2}
+FORMATS = {name: t for name, t in (("e4m3", torch.float8_e4m3fn), ("int8", torch.int8), ("e2m1", paged.E2M1)) if t in paged.FORMATS}
 
 
 class Decoder:

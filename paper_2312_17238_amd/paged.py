@@ -22,7 +22,10 @@ import torch
 from . import binding as B
 
 DTYPES = {torch.float16: B.MOE_KV_F16, torch.bfloat16: B.MOE_KV_BF16}
-FORMATS = {torch.float8_e4m3fn: B.MOE_KV_E4M3, torch.int8: B.MOE_KV_INT8, torch.float4_e2m1fn_x2: B.MOE_KV_E2M1}
+E2M1, E8M0 = getattr(torch, "float4_e2m1fn_x2", None), getattr(torch, "float8_e8m0fnu", None)     # a torch without them keeps caches in 8 bits
+FORMATS = {torch.float8_e4m3fn: B.MOE_KV_E4M3, torch.int8: B.MOE_KV_INT8}
+if E2M1 is not None and E8M0 is not None:
+    FORMATS[E2M1] = B.MOE_KV_E2M1
 
 # A call costs the host a few microseconds, which for single tokens is what counts: structures and references to them are made once,
 # messages only when something is refused.
@@ -82,11 +85,11 @@ class Cache:
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
         _need(k.dtype in FORMATS and v.dtype == k.dtype, f"Cache: codes of type {k.dtype} and {v.dtype}")
-        four = k.dtype is torch.float4_e2m1fn_x2
+        four = k.dtype is E2M1
         if four:
             _need(k.dim() == 4, f"Cache: k has shape {tuple(k.shape)}")
             p, h, page, d = k.shape[0], k.shape[1], k.shape[2], 2 * k.shape[3]
-            scales, kind = ((p, h, page // 16, 4, d // 32, 4), (p, h, page)), torch.float8_e8m0fnu
+            scales, kind = ((p, h, page // 16, 4, d // 32, 4), (p, h, page)), E8M0
             _need(tuple(v.shape) == (p, h, page // 16, d, 8), f"Cache: v has shape {tuple(v.shape)}")
         else:
             _need(k.dim() == 6 and k.shape[4:] == (16, 16), f"Cache: k has shape {tuple(k.shape)}")
@@ -105,13 +108,13 @@ class Cache:
     @classmethod
     def empty(cls, n_pages: int, kv_heads: int, head_dim: int, page: int = 64, dtype=torch.float8_e4m3fn, device="cuda:0") -> "Cache":
         """Uninitialised: a page's content counts from the first token that is written into it."""
+        _need(dtype in FORMATS, f"Cache: codes of type {dtype}")
         _need(page % 16 == 0 and head_dim % 16 == 0, "Cache: page and head_dim have to be multiples of 16")
         b = lambda *shape: torch.empty(*shape, dtype=torch.uint8, device=device)  # noqa: E731
-        if dtype is torch.float4_e2m1fn_x2:
+        if dtype is E2M1:
             _need(head_dim % 32 == 0, "Cache: head_dim has to be a multiple of 32")
-            scale = torch.float8_e8m0fnu
             return cls(b(n_pages, kv_heads, page, head_dim // 2).view(dtype), b(n_pages, kv_heads, page // 16, head_dim, 8).view(dtype),
-                       b(n_pages, kv_heads, page // 16, 4, head_dim // 32, 4).view(scale), b(n_pages, kv_heads, page).view(scale))
+                       b(n_pages, kv_heads, page // 16, 4, head_dim // 32, 4).view(E8M0), b(n_pages, kv_heads, page).view(E8M0))
         k = b(n_pages, kv_heads, page // 16, head_dim // 16, 16, 16)
         v = b(n_pages, kv_heads, page // 16, head_dim, 16)
         s = torch.empty(2, n_pages, kv_heads, dtype=torch.float32, device=device)
