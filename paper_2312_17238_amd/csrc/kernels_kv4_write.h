@@ -96,7 +96,6 @@ __device__ __forceinline__ float tame8(float (&x)[8], float huge)
     return most;
 }
 
-template <int DTYPE>
 __device__ __forceinline__ uint4 load_raw8(const void *base, int64_t at, bool vec)
 {
     const uint16_t *p = static_cast<const uint16_t *>(base) + at;
@@ -150,7 +149,7 @@ __global__ void __launch_bounds__(WRITE_THREADS) k_kv4_write(Write4Args b)
     auto fetch = [&](int r) {
         r = min(r, rows - 1);
         const int t = token_of(r), hh = r - t * hg;
-        return load_raw8<DTYPE>(src, (row0 + t) * stride + (int64_t)(h0 + hh) * D + d0, vec);
+        return load_raw8(src, (row0 + t) * stride + (int64_t)(h0 + hh) * D + d0, vec);
     };
     uint4 next = fetch(mine);
 
@@ -170,8 +169,8 @@ __global__ void __launch_bounds__(WRITE_THREADS) k_kv4_write(Write4Args b)
         const uint32_t one = to_bits<DTYPE>(1.f) * 0x10001u;
         uint4 gain = make_uint4(one, one, one, one), pgain = gain;      // of the dims and of their partners
         if (a.r.eps > 0.f && a.r.k_gamma) {
-            gain = load_raw8<DTYPE>(a.r.k_gamma, d0, false);
-            pgain = load_raw8<DTYPE>(a.r.k_gamma, p0, false);
+            gain = load_raw8(a.r.k_gamma, d0, false);
+            pgain = load_raw8(a.r.k_gamma, p0, false);
         }
         for (int r0 = 0; r0 < rows; r0 += per_pass) {
             const uint4 raw = next;

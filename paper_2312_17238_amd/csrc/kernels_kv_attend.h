@@ -461,8 +461,8 @@ __device__ __forceinline__ void join_sums(const AttendArgs &a, const Item &it, i
     }
 }
 
-// o: outputs [part][kv head][tile_rows][D], ml: [part][kv head][tile_rows][2].  AHEAD: parts of a thread on their way at a time.
-template <int DTYPE, int D, int AHEAD = D == 64 ? 8 : 16>
+// o: outputs [part][kv head][tile_rows][D], ml: [part][kv head][tile_rows][2]
+template <int DTYPE, int D>
 __device__ __forceinline__ void join_parts(const AttendArgs &a, const Item &it, int head, const float *o, const float *ml, int tile_rows, JoinShared &sh)
 {
     constexpr int THREADS = 64 * ATTEND_WAVES;
@@ -474,7 +474,7 @@ __device__ __forceinline__ void join_parts(const AttendArgs &a, const Item &it, 
     auto at = [&](int p, int r) { return (uint32_t)(((it.part0 + p) * heads + head) * tile_rows + r); };
     // Four dims a thread; where that leaves threads over, the parts are dealt out to groups of threads.  The loads are past the
     // caches, one or two microseconds each: the first parts' are on their way before the maxima are known.
-    constexpr int QUADS = D / 4;
+    constexpr int QUADS = D / 4, AHEAD = D == 64 ? 8 : 16;
     const int all = pow2 * QUADS, groups = max(1, THREADS / all);
     const int e_first = groups > 1 ? tid % all : tid, g = groups > 1 ? tid / all : 0;
     float m[AHEAD];
