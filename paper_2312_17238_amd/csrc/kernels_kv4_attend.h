@@ -16,11 +16,11 @@
 // times 2^(128 - b).  b is from 82 to 172, so neither leaves fp32.  b - 128 is the byte with its highest bit turned over, as a signed one: t is of the size of the score
 // and of the scale's exponent, and rounded as numbers of that size are (with b itself, which needs no turning over, by 2^-17 even where both are small).
 //
-// A prompt of 4096 (32 query and 8 kv heads of 128): 166 us, 0.83 PFLOP/s, 71 % of a large library product, by 8-bit codes 163 to 173.  Every wave reads
+// A prompt of 4096 (32 query and 8 kv heads of 128): 164 to 174 us, 0.8 PFLOP/s, 70 % of a large library product, by 8-bit codes the same.  Every wave reads
 // its keys and values for itself, 133 bytes a token and head, out of the caches; nothing is shared through LDS and no wave waits for another.  By way of
 // LDS (keys as they are, values converted once to fp16, scales as numbers) the same prompt took 174 us, with heads of 256 459 instead
-// of 393.  Vector unit 69 % of the time, matrix unit 34 %: the two hardly overlap at two waves a SIMD, so what a step's 195 vector
-// instructions are is what it costs: 32 conversions of values, 44 for bytes and inverses of scales, 16 each of scale, difference, exponential and sum.
+// of 393.  Vector unit 69 % of the time, matrix unit 34 %: the two hardly overlap at two waves a SIMD, so what a step's 198 vector
+// instructions are is what it costs: 32 conversions of values, 48 for bytes and inverses of scales, 16 each of scale, difference, exponential and sum.
 #pragma once
 #include "kernels_kv_attend.h"
 

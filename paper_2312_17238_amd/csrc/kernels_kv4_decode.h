@@ -19,7 +19,9 @@ namespace kv {
 
 // Joining the parts of a tile's rows, in the parts' order.  What this costs is not its bytes but one wait behind the other, those for code that is not in
 // the instruction cache among them: one short loop without a branch inside, which takes a part's maximum, sum and outputs in one go.  One token over 2000
-// (3 parts) takes 11.3 us, 12.0 with join_parts, whose loops are unrolled; over 131000 (64 parts) 36.7 and 38.6; without any join 8.7 and 29.
+// (3 parts) takes 11.3 us, 12.0 with join_parts, whose loops are unrolled; over 131000 (64 parts) 36.7 and 38.6; without any join 8.7 and 29.  SPAN, the parts
+// that a thread asks for at once, as 8, 16 and 32: one token over 2000 10.3, 11.0 and 12.5 us, over 131000 38.5, 38.4 and 38.1, 64 uneven requests 50.0, 51.7
+// and 55.7, 16 of heads of 256 21.2, 21.1 and 24.2.
 struct Join4Shared {
     float4 sum[64 * DECODE_WAVES];      // of a thread
     float2 ml[64 * DECODE_WAVES];

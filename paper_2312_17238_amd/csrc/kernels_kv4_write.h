@@ -12,7 +12,7 @@
 // Prompts of 8 thousand tokens (165 MB, 32 and 8 heads of 128) 54 us, 3.1 TB/s where a large copy has 5.1; 256 tokens 7, one 4.  Queries are 41 of the
 // 54 (fp64's registers leave them half the waves), keys 15.  Queries in a launch of their own, of twice the waves: 30 + 28.6.  Keys in fp32 with a
 // bound on its error, and fp64 only where a code or a scale is in doubt: no faster (the sums of both ends cost what fp64 does), 256 tokens 10.  Registers
-// limited to 80 and 64: 57 and 69.
+// limited to 80 and 64: 57 and 69.  32, 64 and 128 rows a block that stores: 8 thousand tokens stored and read back 68.5, 66.7 and 67.0, 256 and one the same.
 #pragma once
 #include "kernels_kv_write.h"
 

@@ -13,7 +13,7 @@
 // the weight of a value's code is 2^(t - m), m the running maximum of t over the row: scales cost one multiply-add a score, and
 // the weights stay below 2^8 (see RISE) whatever the scales are, as fp16 wants it.  The sum of the probabilities is that of the weights, divided by vs page
 // by page, in fp32 as are scores, maxima and outputs; where value scales lie so far apart that a weight may be too small for fp32 and its
-// probability matter, the probabilities' exponentials are worked out for themselves (see WIDE).  Weights are rounded to fp16 (2^-11 of a weight at most, as an fp16 output is);
+// probability matter, the probabilities' exponentials are worked out for themselves (see WIDE).  Weights are rounded to fp16 (2^-11 of a weight, as an fp16 output is, or 2^-25 of the largest if that is more);
 // bf16 queries become fp16 after a power of two is taken off each row.
 #pragma once
 #include "kernels_kv_common.h"
