@@ -1,5 +1,5 @@
 """Attention over the cache in 4 bits where numbers are far apart: blocks of a query, scores that are large, single tokens beside very many, and what is left of a score's
-last bits. Every form of it: single tokens, tiles of few rows, tiles of many."""
+last bits; rows that see all tokens or none; what the format costs. Every form of it: single tokens, tiles of few rows, tiles of many."""
 import math
 
 import numpy as np
