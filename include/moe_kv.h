@@ -169,9 +169,10 @@ typedef struct {
  * Scores, maxima, sums and outputs are held in fp32, codes are exact.  Rounded to fewer bits are: the weights that values are multiplied with, to fp16
  * (2^-11 of a weight at most; with fp16 outputs the distance from 64 bits is 1.3 times that of fp32 weights, with bf16 outputs the same.  A weight, which is a
  * probability times its value's scale, that is below 2^-14 of the largest that a wave has met is off by 2^-25 of the largest instead, in 4 bits one
- * below 2^-21 by 2^-32: n tokens far behind one lose n times that of the output), and bf16 queries, to fp16 after a power of two is taken off each row (what is 2^38 below a row's largest is dropped).  Both let the matrix units
- * work on 16-bit operands.  With a cache in 4 bits queries of either type are rounded to 21 bits: a number is off by 2^-20 of the
- * power of two above the largest of its 32 dims (0..31, 32..63, ...) at most, which is nothing for those above 2^-9 of it in fp16 and 2^-12 in bf16
+ * below 2^-21 by 2^-32: n tokens far behind one lose n times that of the output), and bf16 queries, to fp16 after a power of two is taken off each row (what is
+ * 2^38 below a row's largest is dropped).  Both let the matrix units work on 16-bit operands.  With a cache in 4 bits queries of either type are rounded
+ * to 21 bits: a number is off by 2^-20 of the power of two above the largest of its 32 dims (0..31, 32..63, ...) at most, which is nothing for those
+ * above 2^-9 of it in fp16 and 2^-12 in bf16
  * (of 2^-99 of the row's largest number where those dims' is smaller still).
  * (fp16 outputs are 2.2 to 2.4e-4 from 64 bits where fp32 throughout is 1.9 to 2.0e-4, single small calls up to 2.5e-4, bf16 ones the same.)  A row whose query holds an infinity or NaN is NaN. */
 int32_t moe_kv_attend(const moe_kv_cache_t *cache, const moe_kv_step_t *step, const void *plan_dev, const int32_t *block_table,
